@@ -44,6 +44,16 @@
  *     v_pool: [n_pages][n_kv_heads][head_dim][16 tokens]  bf16   (transposed inside the page)
  *   page_table[s][j] is the pool page holding logical positions 16j..16j+15 of sequence s.
  *   Use laps_kv_scatter / laps_kv_gather to move token-major K/V in and out of pools.
+ *
+ * 4-bit K/V cache (laps_kv4_*, laps_attention_kv4): the same pages in 17/64 of the bytes.  32 values along head_dim of one token and kv
+ *   head share a scale 2^e, kept as the byte e + 127; each value is a 4-bit float, sign and magnitude 0, .5, 1, 1.5, 2, 3, 4 or 6.
+ *   Written as e = the smallest integer with max|x| <= 7 * 2^e, cut to [-126, 125], and x / 2^e rounded to nearest, ties to the even
+ *   code, magnitudes above 6 to 6: off by at most half the step at the value, a value above 7 * 2^125 by more.  A group with an
+ *   infinity or a NaN gets the byte 255 and reads back as NaN.  Reading back is exact in bf16.
+ *     k4_pool: [n_pages][n_kv_heads] blocks of laps_kv4_block_bytes(head_dim) = 8.5 * head_dim bytes:
+ *              codes [16 tokens][head_dim / 2 bytes], then scales [16 tokens][head_dim / 32]
+ *     v4_pool: blocks of the same size: codes [head_dim / 8][16 tokens][4 bytes], then scales [head_dim / 32][16 tokens]
+ *   two codes a byte, the lower head_dim index in the lower half.  Slots that nothing was written to may hold any bytes.
  */
 #ifndef LAPS_H
 #define LAPS_H
@@ -165,6 +175,18 @@ int laps_kv_scatter(laps_ctx* ctx, int32_t n_seq, int32_t n_tokens, const int32_
 int laps_kv_gather(laps_ctx* ctx, int32_t n_seq, int32_t n_tokens, const int32_t* cu_dev,
                    const int32_t* start_pos_dev, const int32_t* page_table_dev, int32_t max_pages,
                    const void* k_pool_dev, const void* v_pool_dev, void* k_dst_dev, void* v_dst_dev, void* stream);
+
+/* The same moves between token-major bf16 K/V and 4-bit pools (format: above): laps_kv4_scatter quantises what it writes,
+ * laps_kv4_gather reads back.  Tokens whose page is unset, outside the table or outside the pools are not moved; rows outside
+ * [cu_dev[0], cu_dev[n_seq]) and slots of other tokens are left as they were.  Everything but the int32 arrays must be
+ * 16-byte aligned and the context's device current (EINVAL); n_tokens may be 0. */
+size_t laps_kv4_block_bytes(int32_t head_dim); /* 0 if not 64 or 128 */
+int laps_kv4_scatter(laps_ctx* ctx, int32_t n_seq, int32_t n_tokens, const int32_t* cu_dev, const int32_t* start_pos_dev,
+                     const int32_t* page_table_dev, int32_t max_pages, const void* k_src_dev, const void* v_src_dev,
+                     void* k4_pool_dev, void* v4_pool_dev, void* stream);
+int laps_kv4_gather(laps_ctx* ctx, int32_t n_seq, int32_t n_tokens, const int32_t* cu_dev, const int32_t* start_pos_dev,
+                    const int32_t* page_table_dev, int32_t max_pages, const void* k4_pool_dev, const void* v4_pool_dev,
+                    void* k_dst_dev, void* v_dst_dev, void* stream);
 
 /* ------------------------------------------------------------------ prefill forward
  * One decoder layer over a packed ragged batch (Section 2.1: L new tokens attending to H cached
@@ -294,6 +316,20 @@ int laps_attention(laps_ctx* ctx, int32_t n_seq, int32_t n_tokens, const int32_t
                    const int32_t* seq_len_dev, const int32_t* prefix_len_dev, const int32_t* page_table_dev,
                    int32_t max_pages, const void* k_pool_dev, const void* v_pool_dev, const void* q_dev,
                    void* out_dev, void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/* laps_attention over 4-bit pools, from one new token per sequence (a decode step) to chunks of long prompts: q_dev and
+ * out_dev bf16 [n_tokens, n_q*hd], K/V of prefix and new tokens already in the pools (laps_kv4_scatter).  Sequences, lengths,
+ * page table and their bounds as for laps_attention; a sequence may own no rows or have no new token.  Rows of out_dev that hold
+ * no token are left as they were.  A NaN that the cache holds reaches the rows that see its key and no other: of the whole head if
+ * it is K's, of the group's 32 values if it is V's.  workspace_dev: laps_attention_kv4_workspace_bytes(ctx, n_seq, n_tokens,
+ * max_pages) bytes (0 on bad arguments), 256-byte aligned, for this call alone until its work is done.  EINVAL as for laps_attention, and
+ * on pools, q or out that are not 16-byte aligned, more than 2^26 pages a table row, more than 2^20 sequences times query heads, or if the
+ * context's device is not current; ENOMEM if the workspace is too small. */
+size_t laps_attention_kv4_workspace_bytes(const laps_ctx* ctx, int32_t n_seq, int32_t n_tokens, int32_t max_pages);
+int laps_attention_kv4(laps_ctx* ctx, int32_t n_seq, int32_t n_tokens, const int32_t* cu_seqlens_dev,
+                       const int32_t* seq_len_dev, const int32_t* prefix_len_dev, const int32_t* page_table_dev,
+                       int32_t max_pages, const void* k4_pool_dev, const void* v4_pool_dev, const void* q_dev,
+                       void* out_dev, void* workspace_dev, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------ per-kernel timing
  * When enabled, un-captured laps_prefill_* calls bracket every kernel launch with HIP events on

@@ -55,6 +55,8 @@ def lib():
         L.laps_workspace_bytes_for.restype = C.c_size_t
         L.laps_gemm_workspace_bytes.restype = C.c_size_t
         L.laps_static_scratch_bytes.restype = C.c_size_t
+        L.laps_kv4_block_bytes.restype = C.c_size_t
+        L.laps_attention_kv4_workspace_bytes.restype = C.c_size_t
         L.laps_graph_device_bytes.restype = C.c_size_t
         L.laps_graph_output.restype = C.c_void_p
         L.laps_graph_input.restype = C.c_void_p
@@ -117,6 +119,20 @@ def _after_current(stream):
     cur = torch.cuda.current_stream()
     if cur.cuda_stream != stream.cuda_stream and not lib().laps_stream_idle(C.c_void_p(cur.cuda_stream), C.c_void_p(stream.cuda_stream)):
         stream.wait_stream(cur)
+
+
+def _held_by(stream, *tensors):
+    """Tensors made on the current stream for work on `stream`: their memory goes to nobody else before that is done."""
+    if stream is not None and stream.cuda_stream != torch.cuda.current_stream().cuda_stream:
+        for t in tensors:
+            t.record_stream(stream)
+
+
+def _expect(what, t, dtype, *shape):
+    """Refuses a tensor that a kernel would read past or misread; None in `shape` stands for any size."""
+    if not t.is_cuda or t.dtype != dtype or not t.is_contiguous() or t.dim() != len(shape) or any(
+            n is not None and n != m for n, m in zip(shape, t.shape)):
+        raise LapsError(f"{what}: need a contiguous {dtype} device tensor of shape {list(shape)}, got {t.dtype} {list(t.shape)} on {t.device}")
 
 
 def _i32(a):
@@ -440,6 +456,75 @@ class LapsCtx:
         _check(lib().laps_kv_gather(self._h, C.c_int32(n_seq), C.c_int32(n_tokens), _p(cu), _p(start_pos), _p(page_table),
                                     C.c_int32(page_table.shape[1]), _p(k_pool), _p(v_pool), _p(k), _p(v), _stream(stream)))
         return k, v
+
+    # ---- 4-bit KV pools
+    def new_kv4_pools(self, n_pages: int, n_layers: int | None = None, zero: bool = False):
+        mk = torch.zeros if zero else torch.empty
+        shape = (n_pages, self.cfg.n_kv_heads, int(lib().laps_kv4_block_bytes(C.c_int32(self.cfg.head_dim))))
+        k4, v4 = ([mk(shape, dtype=torch.uint8, device="cuda") for _ in range(n_layers or self.cfg.n_layers)] for _ in range(2))
+        return k4, v4
+
+    def _expect_kv4(self, cu, per_seq, page_table, k4_pool, v4_pool):
+        """Shapes of a call on 4-bit pools; returns the number of sequences."""
+        n_seq = cu.numel() - 1
+        _expect("cu", cu, torch.int32, n_seq + 1)
+        for what, t in per_seq.items():
+            if t is not None:
+                _expect(what, t, torch.int32, n_seq)
+        _expect("page_table", page_table, torch.int32, n_seq, None)
+        block = int(lib().laps_kv4_block_bytes(C.c_int32(self.cfg.head_dim)))
+        _expect("k4_pool", k4_pool, torch.uint8, None, self.cfg.n_kv_heads, block)
+        _expect("v4_pool", v4_pool, torch.uint8, k4_pool.shape[0], self.cfg.n_kv_heads, block)
+        if len({t.device for t in (cu, page_table, k4_pool, v4_pool, *(t for t in per_seq.values() if t is not None))}) > 1:
+            raise LapsError("arrays of one call on different devices")
+        return n_seq
+
+    def laps_kv4_scatter(self, cu, start_pos, page_table, k_src, v_src, k4_pool, v4_pool, stream=None):
+        """Quantises token-major bf16 K/V [n_tokens, n_kv_heads, head_dim] into 4-bit pools (new_kv4_pools)."""
+        n_seq, n_tok = self._expect_kv4(cu, {"start_pos": start_pos}, page_table, k4_pool, v4_pool), k_src.shape[0]
+        for what, t in (("k_src", k_src), ("v_src", v_src)):
+            _expect(what, t, torch.bfloat16, n_tok, self.cfg.n_kv_heads, self.cfg.head_dim)
+        self._guard_pools(k4_pool)
+        _after_current(stream)
+        _check(lib().laps_kv4_scatter(self._h, C.c_int32(n_seq), C.c_int32(n_tok), _p(cu), _p(start_pos), _p(page_table),
+                                      C.c_int32(page_table.shape[1]), _p(k_src), _p(v_src), _p(k4_pool), _p(v4_pool), _stream(stream)))
+
+    def laps_kv4_gather(self, cu, start_pos, page_table, k4_pool, v4_pool, n_tokens, k_out=None, v_out=None, stream=None):
+        """Reads token-major bf16 K/V back from 4-bit pools, into k_out / v_out if given.  Rows without a page keep what they
+        held (nothing defined in tensors made here)."""
+        n_seq = self._expect_kv4(cu, {"start_pos": start_pos}, page_table, k4_pool, v4_pool)
+        shp = (n_tokens, self.cfg.n_kv_heads, self.cfg.head_dim)
+        outs = [torch.empty(shp, dtype=torch.bfloat16, device=k4_pool.device) if t is None else t for t in (k_out, v_out)]
+        for what, t in zip(("k_out", "v_out"), outs):
+            _expect(what, t, torch.bfloat16, *shp)
+        self._guard_pools(k4_pool)
+        _after_current(stream)
+        _check(lib().laps_kv4_gather(self._h, C.c_int32(n_seq), C.c_int32(n_tokens), _p(cu), _p(start_pos), _p(page_table),
+                                     C.c_int32(page_table.shape[1]), _p(k4_pool), _p(v4_pool), _p(outs[0]), _p(outs[1]), _stream(stream)))
+        _held_by(stream, *(t for t, given in zip(outs, (k_out, v_out)) if given is None))
+        return outs[0], outs[1]
+
+    def laps_attention_kv4_workspace_bytes(self, n_seq: int, n_tokens: int, max_pages: int) -> int:
+        return int(lib().laps_attention_kv4_workspace_bytes(self._h, C.c_int32(n_seq), C.c_int32(n_tokens), C.c_int32(max_pages)))
+
+    def laps_attention_kv4(self, cu, seq_len, prefix_len, page_table, k4_pool, v4_pool, q, out=None, stream=None):
+        """laps_attention over 4-bit pools.  Rows of `out` that hold no token keep what they held (zeros if made here).  The
+        workspace is this call's own: calls on several streams and captured graphs do not share one."""
+        n_seq = self._expect_kv4(cu, {"seq_len": seq_len, "prefix_len": prefix_len}, page_table, k4_pool, v4_pool)
+        n_tok, width = q.shape[0], self.cfg.n_q_heads * self.cfg.head_dim
+        _expect("q", q, torch.bfloat16, n_tok, width)
+        made = out is None
+        out = torch.zeros_like(q) if made else out
+        _expect("out", out, torch.bfloat16, n_tok, width)
+        need = self.laps_attention_kv4_workspace_bytes(n_seq, n_tok, page_table.shape[1])
+        ws = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+        self._guard_pools(k4_pool)
+        _after_current(stream)
+        _check(lib().laps_attention_kv4(self._h, C.c_int32(n_seq), C.c_int32(n_tok), _p(cu), _p(seq_len), _p(prefix_len),
+                                        _p(page_table), C.c_int32(page_table.shape[1]), _p(k4_pool), _p(v4_pool), _p(q), _p(out),
+                                        _p(ws), C.c_size_t(ws.numel()), _stream(stream)))
+        _held_by(stream, ws, *((out,) if made else ()))
+        return out
 
     # ---- forward
     def laps_prefill_layer(self, w: dict, cu, seq_len, prefix_len, page_table, k_pool, v_pool, x_in, x_out=None,

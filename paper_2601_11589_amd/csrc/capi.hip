@@ -9,6 +9,7 @@
 #include <new>
 #include <vector>
 
+#include "kv4.h"
 #include "laps_internal.h"
 
 // ----------------------------------------------------------------------------- errors
@@ -571,6 +572,87 @@ extern "C" int laps_kv_gather(laps_ctx* c, int32_t n_seq, int32_t n_tokens, cons
                               void* v_dst, void* stream) {
     return kv_move(false, c, n_seq, n_tokens, cu, start_pos, pt, max_pages, k_dst, v_dst, const_cast<void*>(k_pool),
                    const_cast<void*>(v_pool), stream);
+}
+
+// ----------------------------------------------------------------------------- 4-bit cache
+// The kernels run on the current device with addresses of the context's: they must be the same one.
+static int check_current_device(const laps_ctx* c, const char* who) {
+    int dev = -1;
+    if (hipGetDevice(&dev) != hipSuccess || dev != c->device) {
+        laps_set_error("%s: the context's device %d must be current (current: %d)", who, c->device, dev);
+        return LAPS_EINVAL;
+    }
+    return LAPS_OK;
+}
+
+extern "C" size_t laps_kv4_block_bytes(int32_t head_dim) {
+    return head_dim == 64 || head_dim == 128 ? (size_t)kv4_block(head_dim) : 0;
+}
+
+static int kv4_move(bool scatter, laps_ctx* c, int n_seq, int n_tokens, const int* cu, const int* start_pos, const int* pt,
+                    int max_pages, void* k_tok, void* v_tok, void* k_pool, void* v_pool, void* stream) {
+    if (!c || n_seq < 1 || n_tokens < 0 || !cu || !start_pos || !pt || max_pages < 1 || max_pages > LAPS_KV4_MAX_PAGES || !k_pool || !v_pool ||
+        (n_tokens > 0 && (!k_tok || !v_tok))) {
+        laps_set_error("kv4 move: NULL pointer or bad size");
+        return LAPS_EINVAL;
+    }
+    if (((uintptr_t)k_tok | (uintptr_t)v_tok | (uintptr_t)k_pool | (uintptr_t)v_pool) & 15) {
+        laps_set_error("kv4 move: K/V rows and pools must be 16-byte aligned");
+        return LAPS_EINVAL;
+    }
+    LAPS_TRY(check_current_device(c, "kv4 move"));
+    return laps_launch_kv4_move(scatter, n_seq, n_tokens, cu, start_pos, pt, max_pages, k_tok, v_tok, k_pool, v_pool,
+                                c->cfg.n_kv_heads, c->cfg.head_dim, c->pool_pages, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int laps_kv4_scatter(laps_ctx* c, int32_t n_seq, int32_t n_tokens, const int32_t* cu, const int32_t* start_pos,
+                                const int32_t* pt, int32_t max_pages, const void* k_src, const void* v_src, void* k_pool,
+                                void* v_pool, void* stream) {
+    return kv4_move(true, c, n_seq, n_tokens, cu, start_pos, pt, max_pages, const_cast<void*>(k_src), const_cast<void*>(v_src),
+                    k_pool, v_pool, stream);
+}
+
+extern "C" int laps_kv4_gather(laps_ctx* c, int32_t n_seq, int32_t n_tokens, const int32_t* cu, const int32_t* start_pos,
+                               const int32_t* pt, int32_t max_pages, const void* k_pool, const void* v_pool, void* k_dst,
+                               void* v_dst, void* stream) {
+    return kv4_move(false, c, n_seq, n_tokens, cu, start_pos, pt, max_pages, k_dst, v_dst, const_cast<void*>(k_pool),
+                    const_cast<void*>(v_pool), stream);
+}
+
+extern "C" size_t laps_attention_kv4_workspace_bytes(const laps_ctx* c, int32_t n_seq, int32_t n_tokens, int32_t max_pages) {
+    if (!c || n_seq < 1 || n_tokens < 1 || max_pages < 1 || max_pages > LAPS_KV4_MAX_PAGES || (long)n_seq * c->cfg.n_q_heads > LAPS_KV4_MAX_SEQ_HEADS)
+        return 0;
+    const Kv4RowsPlan p = laps_kv4_rows_plan(n_seq, n_tokens, c->cfg.n_q_heads, c->cfg.n_kv_heads, max_pages);
+    return align256(laps_kv4_rows_bytes(p, n_tokens, c->cfg.n_q_heads, c->cfg.head_dim) + 1);
+}
+
+extern "C" int laps_attention_kv4(laps_ctx* c, int32_t n_seq, int32_t n_tokens, const int32_t* cu, const int32_t* seq_len,
+                                  const int32_t* prefix_len, const int32_t* pt, int32_t max_pages, const void* k_pool,
+                                  const void* v_pool, const void* q, void* out, void* ws, size_t ws_bytes, void* stream) {
+    if (!c || n_seq < 1 || n_tokens < 1 || !cu || !prefix_len || !pt || max_pages < 1 || !k_pool || !v_pool || !q || !out || !ws) {
+        laps_set_error("attention_kv4: NULL pointer or bad size");
+        return LAPS_EINVAL;
+    }
+    const size_t need = laps_attention_kv4_workspace_bytes(c, n_seq, n_tokens, max_pages);
+    if (need == 0) {
+        laps_set_error("attention_kv4: %d sequences of %d query heads or page tables of %d pages are too many", n_seq,
+                       c->cfg.n_q_heads, max_pages);
+        return LAPS_EINVAL;
+    }
+    if ((((uintptr_t)k_pool | (uintptr_t)v_pool | (uintptr_t)q | (uintptr_t)out) & 15) || ((uintptr_t)ws & 255)) {
+        laps_set_error("attention_kv4: pools, q and out must be 16-byte aligned, the workspace 256-byte");
+        return LAPS_EINVAL;
+    }
+    LAPS_TRY(check_current_device(c, "attention_kv4"));
+    if (ws_bytes < need) {
+        laps_set_error("attention_kv4: workspace too small (%zu < %zu bytes)", ws_bytes, need);
+        return LAPS_ENOMEM;
+    }
+    const Kv4Attn a = {static_cast<const bf16_t*>(q), static_cast<bf16_t*>(out), static_cast<const unsigned char*>(k_pool),
+                       static_cast<const unsigned char*>(v_pool), cu, seq_len, prefix_len, pt, n_seq, n_tokens, max_pages,
+                       c->pool_pages, c->cfg.n_q_heads, c->cfg.n_kv_heads, c->cfg.head_dim};
+    const Kv4RowsPlan p = laps_kv4_rows_plan(n_seq, n_tokens, a.n_q, a.n_kv, max_pages);
+    return laps_launch_kv4_rows(a, p, p.parts > 1 ? static_cast<float*>(ws) : nullptr, static_cast<hipStream_t>(stream));
 }
 
 extern "C" size_t laps_gemm_workspace_bytes(int32_t m, int32_t n, int32_t k, int32_t split_k) {

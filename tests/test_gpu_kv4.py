@@ -1,0 +1,441 @@
+"""laps_kv4_scatter / laps_kv4_gather bit for bit against the definition, laps_attention_kv4 element by element against it in 64
+bits, and the three together as a server would call them."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv4_oracle as O
+from paper_2601_11589_amd import api, inputs
+
+pytestmark = pytest.mark.gpu
+ULP = 2.0 ** -8      # half a step of bf16, relative
+
+
+def dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a, np.int32)).cuda()
+
+
+def bf16(g, shape):
+    return torch.from_numpy(g.standard_normal(shape).astype(np.float32)).to(torch.bfloat16)
+
+
+def wide(t):
+    return t.double().cpu().numpy()
+
+
+class Batch:
+    """New tokens and cached ones of a few sequences over random pages, on the host and in 4-bit pools full of stale bytes."""
+
+    def __init__(self, cfg, new, pre, seed=1, spare=2, pad=None, ctx=None, low_page=0):
+        self.cfg, self.new, self.pre = cfg, np.asarray(new), np.asarray(pre)
+        self.g = g = np.random.default_rng(seed)
+        self.rows = self.new + (0 if pad is None else np.asarray(pad))
+        self.cu = np.concatenate([[0], np.cumsum(self.rows)]).astype(np.int32)
+        need = -(-(self.new + self.pre) // 16)
+        n_pages = int(need.sum()) + 3
+        order = g.permutation(n_pages)
+        self.table = np.full((len(self.new), int(need.max()) + spare), -1, np.int32)
+        at = 0
+        for i, m in enumerate(need):
+            self.table[i, :m] = order[at:at + m]
+            at += m
+        self.ctx = ctx or api.LapsCtx(cfg, 64)
+        shape = (n_pages, cfg.n_kv_heads, O.block_bytes(cfg.head_dim))
+        self.k4, self.v4 = (torch.from_numpy(g.integers(0, 256, shape).astype(np.uint8)).cuda() for _ in range(2))
+        total = int((self.new + self.pre).sum())
+        self.k, self.v = (bf16(g, (total, cfg.n_kv_heads, cfg.head_dim)) for _ in range(2))
+        self.first = np.concatenate([[0], np.cumsum(self.new + self.pre)])
+        self.q = bf16(g, (int(self.rows.sum()), cfg.n_q_heads * cfg.head_dim))
+
+    def write(self, which="all"):
+        """All tokens, the cached ones or the new ones into the pools, through the library."""
+        lo = self.pre if which == "new" else np.zeros_like(self.pre)
+        n = {"all": self.new + self.pre, "new": self.new, "cached": self.pre}[which]
+        at = np.concatenate([np.arange(f + a, f + a + m) for f, a, m in zip(self.first, lo, n)]).astype(np.int64)
+        self.ctx.laps_kv4_scatter(dev(np.concatenate([[0], np.cumsum(n)])), dev(lo), dev(self.table), self.k[at].cuda(), self.v[at].cuda(),
+                                  self.k4, self.v4)
+        return self
+
+    def attend(self, out=None, padded=None, stream=None):
+        seq_len = dev(self.new) if (self.rows != self.new).any() or padded else None
+        return self.ctx.laps_attention_kv4(dev(self.cu), seq_len, dev(self.pre), dev(self.table), self.k4, self.v4, self.q.cuda(), out, stream)
+
+    def oracle(self):
+        out, spread = (np.zeros((len(self.q), self.cfg.n_q_heads, self.cfg.head_dim)) for _ in range(2))
+        bound = np.zeros((len(self.q), 1, 1))
+        for i, (n, h) in enumerate(zip(self.new, self.pre)):
+            if n == 0:
+                continue
+            at = slice(self.first[i], self.first[i + 1])
+            k, v = (O.value(*O.quantise(wide(t[at]))) for t in (self.k, self.v))
+            r = slice(self.cu[i], self.cu[i] + n)
+            q = wide(self.q[r]).reshape(n, self.cfg.n_q_heads, -1)
+            out[r], spread[r] = O.attend(q, k, v, int(h))
+            # largest sum |q k| of a score: what its float32 sum is off by, in units of 2^-24 a term
+            bound[r] = np.abs(q).max() * np.nanmax(np.abs(k).sum(-1)) * math.sqrt(self.cfg.head_dim)
+        return out, spread, bound
+
+    def check(self, got, oracle=None):
+        """|got - out| <= ULP (sum p|v| + 2 |out|): the weights p, their sum (it may be that of the rounded ones) and the output are
+        rounded to bf16; and a float32 term: a score
+        is off by hd terms of 2^-24, an exponential and the sums by less than 2^-20, which moves the weights by as much."""
+        out, spread, bound = self.oracle() if oracle is None else oracle
+        got = wide(got).reshape(out.shape)
+        live = np.concatenate([np.arange(c, c + n) for c, n in zip(self.cu, self.new)]).astype(int)
+        slack = ULP * (spread + 2 * np.abs(out)) * (1 + 4 * ULP) + 4 * spread * (bound * 2.0 ** -24 + 2.0 ** -20)
+        with np.errstate(invalid="ignore"):
+            bad = ~(np.abs(got - out) <= slack) & ~(np.isnan(got) & np.isnan(out))
+        assert not bad[live].any(), (np.argwhere(bad[live])[:4], got[live][bad[live]][:4], out[live][bad[live]][:4])
+        return live
+
+
+# ------------------------------------------------------------------------------------------------ scatter, gather
+def odd_values(g, shape):
+    """Groups of every size of exponent, with zeros, subnormals, the largest values, infinities and NaN among them."""
+    bits = g.integers(0, 1 << 16, shape).astype(np.uint16)
+    spread = inputs.f32_to_bf16_bits((g.standard_normal(shape) * np.exp2(g.integers(-20, 20, shape[:-1] + (1,)))).astype(np.float32))
+    kind = np.repeat(g.integers(0, 4, shape[:-1] + (shape[-1] // 32,)), 32, -1)
+    bits = np.where(kind == 0, bits, np.where(kind == 1, spread, np.where(kind == 2, bits & 0x80ff, (bits & 0x807f) | 0x7f00)))
+    return torch.from_numpy(bits.astype(np.uint16).view(np.int16)).view(torch.bfloat16)
+
+
+@pytest.mark.parametrize("cfgf", [inputs.tiny_cfg, inputs.qwen7b_cfg])
+@pytest.mark.parametrize("lens,start", [([1], [15]), ([16, 16], [0, 32]), ([17, 0, 3, 40, 1], [5, 9, 14, 31, 0]),
+                                        ([0, 33, 100, 7], [3, 1, 16, 2000]), ([0], [0])])
+def test_pools_hold_the_definition_and_read_back(lens, start, cfgf):
+    cfg = cfgf(1)
+    ctx = api.LapsCtx(cfg, 64)
+    n, rows, g = len(lens), sum(lens), np.random.default_rng(sum(lens) * 7 + 1)
+    table, n_pages = inputs.make_page_table(3, np.asarray(lens) + 1, np.asarray(start))
+    table[n - 1, start[n - 1] // 16] = -1                                  # unset entry: these tokens are not moved
+    cu = np.concatenate([[0], np.cumsum(lens)])
+    k, v = (odd_values(g, (rows, cfg.n_kv_heads, cfg.head_dim)) for _ in range(2))
+    kp, vp = (g.integers(0, 256, (n_pages, cfg.n_kv_heads, O.block_bytes(cfg.head_dim))).astype(np.uint8) for _ in range(2))
+    want_k, want_v = kp.copy(), vp.copy()
+    moved = np.zeros(rows, bool)
+    if rows:
+        quant = O.quantise(wide(k)), O.quantise(wide(v))
+    for i in range(n):
+        for t in range(lens[i]):
+            r, pos = cu[i] + t, start[i] + t
+            if table[i, pos // 16] >= 0:
+                moved[r] = True
+                O.put(want_k, want_v, table[i, pos // 16], pos % 16, quant[0][0][r], quant[0][1][r], quant[1][0][r], quant[1][1][r])
+    k4, v4 = torch.from_numpy(kp).cuda(), torch.from_numpy(vp).cuda()
+    ctx.laps_kv4_scatter(dev(cu), dev(start), dev(table), k.cuda(), v.cuda(), k4, v4)
+    assert np.array_equal(k4.cpu().numpy(), want_k) and np.array_equal(v4.cpu().numpy(), want_v)
+    outs = [torch.full((rows, cfg.n_kv_heads, cfg.head_dim), 3.25, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    back = ctx.laps_kv4_gather(dev(cu), dev(start), dev(table), k4, v4, rows, *outs)
+    for i, (got, x) in enumerate(zip(back, (k, v))):
+        assert got is outs[i]
+        if rows:
+            assert np.array_equal(wide(got)[moved], O.value(*O.quantise(wide(x)))[moved], equal_nan=True)
+            assert (wide(got)[~moved] == 3.25).all()
+    ctx.close()
+
+
+def test_every_bf16_value_as_a_group_of_its_own():
+    cfg = inputs.tiny_cfg(1)
+    ctx = api.LapsCtx(cfg, 64)
+    bits = np.arange(1 << 16).astype(np.uint16)
+    x = np.zeros((1 << 16, 32), np.uint16)
+    x[:, 5] = bits                                   # sets the scale
+    x[:, 6:20] = np.clip((bits & 0x7fff)[:, None].astype(int) - np.arange(14) * 23, 0, 0x7fff)      # smaller ones beside it
+    x = torch.from_numpy(x.reshape(-1, cfg.n_kv_heads, cfg.head_dim).view(np.int16)).view(torch.bfloat16)
+    n = x.shape[0]
+    table = dev(np.arange(-(-n // 16))[None])
+    k4, v4 = ctx.new_kv4_pools(table.shape[1], 1)
+    ctx.laps_kv4_scatter(dev([0, n]), dev([0]), table, x.cuda(), x.flip(0).contiguous().cuda(), k4[0], v4[0])
+    k, v = ctx.laps_kv4_gather(dev([0, n]), dev([0]), table, k4[0], v4[0], n)
+    want = O.value(*O.quantise(wide(x)))
+    assert np.array_equal(wide(k), want, equal_nan=True) and np.array_equal(wide(v.flip(0)), want, equal_nan=True)
+    ctx.close()
+
+
+# ------------------------------------------------------------------------------------------------ attention
+SHAPES = [
+    ([1], [0]), ([1], [1]), ([1], [31]), ([1], [127]), ([1], [4001]),                 # a token with more and more behind it
+    ([1] * 9, [0, 15, 16, 17, 300, 1000, 64, 2047, 5]),                               # a decode batch
+    ([3, 0, 1, 5, 2], [0, 7, 500, 33, 1111]),                                         # drafted tokens, one sequence without any
+    ([2], [40]), ([17], [0]), ([16], [1000]), ([33, 1, 64], [100, 3000, 0]),          # short turns
+    ([130], [0]), ([257, 40], [70, 900]), ([0, 0, 1], [5, 0, 9]),
+]
+
+
+@pytest.mark.parametrize("cfgf", [inputs.tiny_cfg, inputs.qwen7b_cfg, inputs.qwen14b_cfg])
+@pytest.mark.parametrize("new,pre", SHAPES)
+def test_attention_matches_the_definition(new, pre, cfgf):
+    b = Batch(cfgf(1), new, pre, seed=sum(new) + sum(pre)).write()
+    b.check(b.attend())
+    b.ctx.close()
+
+
+@pytest.mark.parametrize("spare", [0, 1, 60, 700])
+def test_width_of_the_page_table(spare):
+    b = Batch(inputs.qwen7b_cfg(1), [1, 1, 4], [900, 3, 2500], spare=spare).write()
+    b.check(b.attend())
+    b.ctx.close()
+
+
+@pytest.mark.parametrize("heads", [(8, 8, 64), (1, 1, 128), (16, 1, 128), (34, 2, 64), (6, 2, 128)])
+def test_head_layouts(heads):
+    n_q, n_kv, hd = heads
+    cfg = inputs.ModelCfg(256, n_q, n_kv, hd, 512, 1)
+    b = Batch(cfg, [1, 2, 19], [700, 33, 150], seed=n_q).write()
+    b.check(b.attend())
+    b.ctx.close()
+
+
+def test_many_sequences():
+    g = np.random.default_rng(8)
+    b = Batch(inputs.tiny_cfg(1), g.integers(0, 3, 700), g.integers(0, 90, 700)).write()
+    b.check(b.attend())
+    b.ctx.close()
+
+
+@pytest.mark.parametrize("cfgf", [inputs.tiny_cfg, inputs.qwen14b_cfg])
+@pytest.mark.parametrize("new,pre,pad", [([3, 0, 1, 20], [50, 9, 400, 0], [2, 3, 0, 1]), ([1, 1], [5, 2000], [7, 1]), ([0, 0], [4, 0], [1, 3])])
+def test_rows_without_a_token_stay(new, pre, pad, cfgf):
+    b = Batch(cfgf(1), new, pre, pad=pad).write()
+    out = torch.full((len(b.q) + 5, b.q.shape[1]), 7.5, dtype=torch.bfloat16, device="cuda")
+    b.q = torch.cat([b.q, b.q[:1].expand(5, -1)])       # and rows behind the last sequence
+    live = b.check(b.attend(out))
+    rest = np.setdiff1d(np.arange(len(b.q)), live)
+    assert (out[torch.from_numpy(rest).cuda()] == 7.5).all()
+    b.ctx.close()
+
+
+@pytest.mark.parametrize("cfgf", [inputs.tiny_cfg, inputs.qwen7b_cfg])
+@pytest.mark.parametrize("new,pre,at", [([1, 1], [40, 900], 17), ([1, 1], [900, 700], 899), ([6, 3], [70, 40], 72), ([40, 20], [100, 9], 103),
+                                        ([200, 150], [30, 0], 110), ([6, 3], [70, 40], 0)])
+def test_a_nan_reaches_the_rows_that_see_it(new, pre, at, cfgf):
+    """One V group, then one K group of key `at` of the first sequence not finite."""
+    for which in ("v", "k"):
+        b = Batch(cfgf(1), new, pre, seed=at)
+        (b.v if which == "v" else b.k)[at, 1, 37] = math.inf
+        b.write()
+        want = b.oracle()
+        assert np.isnan(want[0]).any() and not np.isnan(want[0]).all()
+        b.check(b.attend(), want)
+        b.ctx.close()
+
+
+def test_scores_far_apart_and_all_equal():
+    cfg = inputs.qwen7b_cfg(1)
+    for scale in (0.0, 30.0, 1e-30):
+        b = Batch(cfg, [1, 2, 70], [1500, 33, 200])
+        b.q = (b.q.float() * scale).to(torch.bfloat16)
+        b.write()
+        b.check(b.attend())
+        b.ctx.close()
+
+
+def test_a_value_follows_its_own_key():
+    """Keys that only one row's query matches: the output is that key's value to the last bit (all else has weight 2^-100)."""
+    cfg = inputs.tiny_cfg(1)
+    b = Batch(cfg, [5], [300])
+    b.k[:] = 0
+    b.q[:] = 0
+    for t in range(5):
+        b.k[60 * t + 7, :, t] = 4.0
+        b.q.view(5, cfg.n_q_heads, cfg.head_dim)[t, :, t] = 400.0
+    got = wide(b.write().attend()).reshape(5, cfg.n_q_heads, cfg.head_dim)
+    want = O.value(*O.quantise(wide(b.v)))
+    for t in range(5):
+        for h in range(cfg.n_q_heads):
+            assert np.array_equal(got[t, h], want[60 * t + 7, h // 2])
+    b.ctx.close()
+
+
+def test_unset_pages_read_page_zero_and_lengths_are_cut():
+    """What stale arrays can reach: unset and out-of-range ids fall back to page 0, a length to the rows a sequence owns, a
+    prefix to the table's width.  Nothing outside the arrays is touched; rows of whole sequences stay right."""
+    cfg = inputs.qwen7b_cfg(1)
+    b = Batch(cfg, [2, 3, 1], [100, 50, 60], spare=0).write()
+    good = b.table.copy()
+    want = b.oracle()
+    table = good.copy()
+    table[0, 1], table[0, 2], table[0, 3] = -1, 1 << 30, -(1 << 31)
+    out = b.ctx.laps_attention_kv4(dev(b.cu), dev([9, 3, 1]), dev([100, 50, 1 << 30]), dev(table), b.k4, b.v4, b.q.cuda())
+    b.new = np.array([0, 3, 0])
+    b.check(out, want)
+    assert out.shape == b.q.shape
+    b.ctx.close()
+
+
+def test_long_offsets():
+    """Pages at the end of pools of more than 4 GiB, more than 2^16 keys."""
+    cfg = inputs.qwen7b_cfg(1)
+    ctx = api.LapsCtx(cfg, 64)
+    n, pages = 70001, 1 << 20
+    k4, v4 = ctx.new_kv4_pools(pages, 1, zero=True)
+    table = dev((pages - 1 - np.arange(-(-n // 16)))[None])
+    g = torch.Generator(device="cuda").manual_seed(5)
+    k, v = (torch.empty((n, cfg.n_kv_heads, cfg.head_dim), dtype=torch.bfloat16, device="cuda").normal_(0, 1, generator=g) for _ in range(2))
+    q = torch.empty((1, cfg.n_q_heads * cfg.head_dim), dtype=torch.bfloat16, device="cuda").normal_(0, 1, generator=g)
+    ctx.laps_kv4_scatter(dev([0, n]), dev([0]), table, k, v, k4[0], v4[0])
+    rk, rv = ctx.laps_kv4_gather(dev([0, n]), dev([0]), table, k4[0], v4[0], n)
+    few = torch.tensor([0, 1, 40000, n - 1])
+    for got, x in ((rk, k), (rv, v)):
+        assert np.array_equal(wide(got[few]), O.value(*O.quantise(wide(x[few]))))
+    out = ctx.laps_attention_kv4(dev([0, 1]), None, dev([n - 1]), table, k4[0], v4[0], q)
+    want, spread = O.attend(wide(q).reshape(1, cfg.n_q_heads, -1), wide(rk), wide(rv), n - 1)
+    err = np.abs(wide(out).reshape(want.shape) - want)
+    assert (err <= ULP * (spread + 2 * np.abs(want)) * (1 + 4 * ULP) + spread * 2.0 ** -14).all()
+    ctx.close()
+
+
+# ------------------------------------------------------------------------------------------------ together
+@pytest.mark.parametrize("cfgf", [inputs.tiny_cfg, inputs.qwen7b_cfg])
+def test_decode_steps_agree_with_one_chunk(cfgf):
+    """A prompt written and attended to as one chunk, then the same tokens one at a time, each written before it is attended
+    to: what a server does.  Both against the definition; the pools the same to the last byte."""
+    cfg = cfgf(1)
+    b = Batch(cfg, [37, 20], [13, 160])
+    b.write("cached")
+    chunk_k, chunk_v = b.k4.clone(), b.v4.clone()
+    first_k, first_v = b.k4.clone(), b.v4.clone()
+    b.write("new")
+    want = b.oracle()
+    b.check(b.attend(), want)
+    chunk_k, chunk_v = b.k4.clone(), b.v4.clone()
+    b.k4.copy_(first_k), b.v4.copy_(first_v)
+    out = torch.zeros_like(b.q).cuda()
+    for t in range(37):
+        on = [i for i in range(2) if t < b.new[i]]
+        rows = torch.tensor([b.cu[i] + t for i in on])
+        src = torch.tensor([b.first[i] + b.pre[i] + t for i in on])
+        table, pos, cu = dev(b.table[on]), dev([b.pre[i] + t for i in on]), dev(np.arange(len(on) + 1))
+        b.ctx.laps_kv4_scatter(cu, pos, table, b.k[src].cuda(), b.v[src].cuda(), b.k4, b.v4)
+        out[rows.cuda()] = b.ctx.laps_attention_kv4(cu, None, pos, table, b.k4, b.v4, b.q[rows].cuda())
+    assert torch.equal(b.k4, chunk_k) and torch.equal(b.v4, chunk_v)
+    b.check(out, want)
+    b.ctx.close()
+
+
+def test_prefill_cache_goes_on_in_four_bits():
+    """K/V of a bf16 pool (the prefill path's) through laps_kv_gather into 4-bit pools, attention of the next token over them,
+    against attention over bf16 pools that hold the rounded values."""
+    cfg = inputs.qwen7b_cfg(1)
+    b = Batch(cfg, [1, 1], [75, 300])
+    cu, zero = dev(b.first), dev([0, 0])
+    n_pages = b.k4.shape[0]
+    kp, vp = b.ctx.new_pools(n_pages, 1)
+    b.ctx.laps_kv_scatter(cu, zero, dev(b.table), b.k.cuda(), b.v.cuda(), kp[0], vp[0])
+    k, v = b.ctx.laps_kv_gather(cu, zero, dev(b.table), kp[0], vp[0], len(b.k))
+    b.ctx.laps_kv4_scatter(cu, zero, dev(b.table), k, v, b.k4, b.v4)
+    k, v = b.ctx.laps_kv4_gather(cu, zero, dev(b.table), b.k4, b.v4, len(b.k))
+    b.ctx.laps_kv_scatter(cu, zero, dev(b.table), k, v, kp[0], vp[0])
+    want = b.oracle()
+    b.check(b.attend(), want)
+    b.check(b.ctx.laps_attention(dev(b.cu), None, dev(b.pre), dev(b.table), kp[0], vp[0], b.q.cuda()), want)
+    b.ctx.close()
+
+
+# ------------------------------------------------------------------------------------------------ streams, graphs, refusals
+@pytest.mark.parametrize("new,pre", [([1, 1, 1], [700, 20, 3000]), ([40, 30], [500, 900]), ([300], [100])])
+def test_captured_steps_replay_with_new_contents(new, pre):
+    """Two graphs of one step each (write, attend), replayed in turns with other tokens, lengths and queries in between eager calls."""
+    b = Batch(inputs.qwen7b_cfg(1), new, pre).write("cached")
+    cu, table, n = dev(b.cu), dev(b.table), int(b.new.sum())
+    prefix, q = dev(b.pre), b.q.cuda()
+    at = np.concatenate([np.arange(f + p, f + p + m) for f, p, m in zip(b.first, b.pre, b.new)])
+    k, v = b.k[at].cuda(), b.v[at].cuda()
+
+    def step():
+        b.ctx.laps_kv4_scatter(cu, prefix, table, k, v, b.k4, b.v4)
+        return b.ctx.laps_attention_kv4(cu, None, prefix, table, b.k4, b.v4, q)
+
+    step()
+    graphs = []
+    for _ in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = step()
+        graphs.append((graph, out))
+    g = torch.Generator(device="cuda").manual_seed(4)
+    for turn in range(6):
+        for t in (k, v, q):
+            t.normal_(0, 1, generator=g)
+        if turn == 3:
+            prefix.sub_(9)
+        graph, out = graphs[turn % 2]
+        graph.replay()
+        want = step()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.isfinite(want.float()).all()
+    b.ctx.close()
+
+
+def test_two_streams_at_once():
+    cfg = inputs.qwen7b_cfg(1)
+    ctx = api.LapsCtx(cfg, 64)
+    batches = [Batch(cfg, [1] * 6, [900, 40, 2000, 7, 100, 1500], seed=s, ctx=ctx).write() for s in (1, 2)]
+    want = [b.attend() for b in batches]
+    streams = [torch.cuda.Stream() for _ in batches]
+    got = [[b.attend(stream=s) for b, s in zip(batches, streams)] for _ in range(8)]
+    torch.cuda.synchronize()
+    for round_ in got:
+        assert all(torch.equal(a, b) for a, b in zip(round_, want))
+    for b, w in zip(batches, want):
+        b.check(w)
+    ctx.close()
+
+
+def test_results_repeat_and_do_not_depend_on_the_batch():
+    cfg = inputs.qwen14b_cfg(1)
+    b = Batch(cfg, [1] * 5, [3000, 10, 700, 64, 1999]).write()
+    out = b.attend()
+    assert torch.equal(out, b.attend())
+    moved = b.pre.copy()
+    moved[[0, 3]] = [5, 2]                 # other sequences get shorter
+    other = b.ctx.laps_attention_kv4(dev(b.cu), None, dev(moved), dev(b.table), b.k4, b.v4, b.q.cuda())
+    assert torch.equal(out[[1, 2, 4]], other[[1, 2, 4]])
+    b.ctx.close()
+
+
+def test_refusals():
+    cfg = inputs.qwen7b_cfg(1)
+    b = Batch(cfg, [1, 2], [40, 9]).write()
+    cu, pre, table, q = dev(b.cu), dev(b.pre), dev(b.table), b.q.cuda()
+    x = torch.zeros((3, cfg.n_kv_heads, cfg.head_dim), dtype=torch.bfloat16, device="cuda")
+    before = b.k4.clone(), b.v4.clone()
+
+    def refused(f, *args, match, **kw):
+        with pytest.raises(api.LapsError, match=match):
+            f(*args, **kw)
+
+    at, sc, ga = b.ctx.laps_attention_kv4, b.ctx.laps_kv4_scatter, b.ctx.laps_kv4_gather
+    refused(at, cu, None, pre[:1], table, b.k4, b.v4, q, match="prefix_len")
+    refused(at, cu, pre.long(), pre, table, b.k4, b.v4, q, match="seq_len")
+    refused(at, cu, None, pre, table[:1], b.k4, b.v4, q, match="page_table")
+    refused(at, cu, None, pre, table, b.k4[..., :-1], b.v4, q, match="k4_pool")
+    refused(at, cu, None, pre, table, b.k4, b.v4[1:], q, match="v4_pool")
+    refused(at, cu, None, pre, table, b.k4, b.v4, q.float(), match="q:")
+    refused(at, cu, None, pre, table, b.k4, b.v4, q[:, 1:], match="q:")
+    refused(at, cu, None, pre, table, b.k4, b.v4, q, q.float(), match="out")
+    refused(at, cu, None, pre, table, b.k4, b.v4, q[:0], match="bad size")
+    refused(at, cu.cpu(), None, pre, table, b.k4, b.v4, q, match="cu")
+    refused(sc, cu, pre, table, x[:, :1], x, b.k4, b.v4, match="k_src")
+    refused(sc, cu, pre, table, x, x[:2], b.k4, b.v4, match="v_src")
+    refused(ga, cu, pre, table, b.k4, b.v4, 3, x, x.float(), match="v_out")
+    odd = torch.zeros(x.numel() + 1, dtype=torch.bfloat16, device="cuda")[1:].view(x.shape)
+    refused(sc, cu, pre, table, odd, x, b.k4, b.v4, match="aligned")
+    refused(ga, cu, pre, table, b.k4, b.v4, 3, x, odd, match="aligned")
+    odd_q = torch.zeros(q.numel() + 1, dtype=torch.bfloat16, device="cuda")[1:].view(q.shape)
+    refused(at, cu, None, pre, table, b.k4, b.v4, odd_q, match="aligned")
+    need = b.ctx.laps_attention_kv4_workspace_bytes(2, 3, table.shape[1])
+    p = lambda t: C.c_void_p(t.data_ptr())
+    ws = torch.empty(need + 256, dtype=torch.uint8, device="cuda")
+    call = lambda w, n, pages: api.lib().laps_attention_kv4(b.ctx._h, C.c_int32(2), C.c_int32(3), p(cu), None, p(pre), p(table), C.c_int32(pages),
+                                                           p(b.k4), p(b.v4), p(q), p(q), C.c_void_p(w), C.c_size_t(n), None)
+    assert call(ws.data_ptr(), need - 1, table.shape[1]) == -2
+    assert call(ws.data_ptr() + 16, need, table.shape[1]) == -1
+    assert call(ws.data_ptr(), need, (1 << 26) + 1) == -1
+    assert b.ctx.laps_attention_kv4_workspace_bytes(1 << 20, 1 << 20, 4) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(before[0], b.k4) and torch.equal(before[1], b.v4)
+    b.ctx.close()
