@@ -86,6 +86,11 @@ def lib():
         L.laps_plan_free.argtypes = [C.c_void_p]
         L.laps_ctx_destroy.argtypes = [C.c_void_p]
         L.laps_graph_destroy.argtypes = [C.c_void_p]
+        p, i = C.c_void_p, C.c_int32
+        L.laps_kv4_block_bytes.argtypes = [i]
+        L.laps_kv4_scatter.argtypes = L.laps_kv4_gather.argtypes = [p, i, i, p, p, p, i, p, p, p, p, p]
+        L.laps_attention_kv4_workspace_bytes.argtypes = [p, i, i, i]
+        L.laps_attention_kv4.argtypes = [p, i, i, p, p, p, p, i, p, p, p, p, p, C.c_size_t, p]
         _lib = L
     return _lib
 
@@ -129,10 +134,10 @@ def _held_by(stream, *tensors):
 
 
 def _expect(what, t, dtype, *shape):
-    """Refuses a tensor that a kernel would read past or misread; None in `shape` stands for any size."""
-    if not t.is_cuda or t.dtype != dtype or not t.is_contiguous() or t.dim() != len(shape) or any(
-            n is not None and n != m for n, m in zip(shape, t.shape)):
+    """Refuses a tensor that a kernel would read past or misread; returns its address."""
+    if t.dtype is not dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
         raise LapsError(f"{what}: need a contiguous {dtype} device tensor of shape {list(shape)}, got {t.dtype} {list(t.shape)} on {t.device}")
+    return t.data_ptr()
 
 
 def _i32(a):
@@ -373,6 +378,7 @@ class LapsCtx:
         self._h = C.c_void_p()
         _check(lib().laps_ctx_create(C.byref(self._c), C.c_int32(max_positions), C.byref(self._h)))
         self._ws = None
+        self._kv4_block = lib().laps_kv4_block_bytes(cfg.head_dim)
 
     def close(self):
         if self._h:
@@ -460,69 +466,73 @@ class LapsCtx:
     # ---- 4-bit KV pools
     def new_kv4_pools(self, n_pages: int, n_layers: int | None = None, zero: bool = False):
         mk = torch.zeros if zero else torch.empty
-        shape = (n_pages, self.cfg.n_kv_heads, int(lib().laps_kv4_block_bytes(C.c_int32(self.cfg.head_dim))))
+        shape = (n_pages, self.cfg.n_kv_heads, self._kv4_block)
         k4, v4 = ([mk(shape, dtype=torch.uint8, device="cuda") for _ in range(n_layers or self.cfg.n_layers)] for _ in range(2))
         return k4, v4
 
-    def _expect_kv4(self, cu, per_seq, page_table, k4_pool, v4_pool):
-        """Shapes of a call on 4-bit pools; returns the number of sequences."""
-        n_seq = cu.numel() - 1
-        _expect("cu", cu, torch.int32, n_seq + 1)
-        for what, t in per_seq.items():
-            if t is not None:
-                _expect(what, t, torch.int32, n_seq)
-        _expect("page_table", page_table, torch.int32, n_seq, None)
-        block = int(lib().laps_kv4_block_bytes(C.c_int32(self.cfg.head_dim)))
-        _expect("k4_pool", k4_pool, torch.uint8, None, self.cfg.n_kv_heads, block)
-        _expect("v4_pool", v4_pool, torch.uint8, k4_pool.shape[0], self.cfg.n_kv_heads, block)
-        if len({t.device for t in (cu, page_table, k4_pool, v4_pool, *(t for t in per_seq.values() if t is not None))}) > 1:
-            raise LapsError("arrays of one call on different devices")
-        return n_seq
+    def _kv4_call(self, cu, per_seq, page_table, k4_pool, v4_pool):
+        """Checks what every call on 4-bit pools takes; returns the sequences, the table's width, the arrays' addresses and
+        their device."""
+        n_seq, width = cu.numel() - 1, page_table.shape[-1]
+        at = [_expect("cu", cu, torch.int32, n_seq + 1)]
+        at += [0 if t is None else _expect(what, t, torch.int32, n_seq) for what, t in per_seq]
+        at.append(_expect("page_table", page_table, torch.int32, n_seq, width))
+        at += [_expect(what, t, torch.uint8, k4_pool.shape[0], self.cfg.n_kv_heads, self._kv4_block)
+               for what, t in (("k4_pool", k4_pool), ("v4_pool", v4_pool))]
+        return n_seq, width, at, k4_pool.get_device()
+
+    @staticmethod
+    def _same_device(device, *tensors):
+        if any(t is not None and t.get_device() != device for t in tensors):
+            raise LapsError("tensors of one call on different devices")
+
+    def _kv4_stream(self, stream, k4_pool, device):
+        self._guard_pools(k4_pool)
+        _after_current(stream)
+        return (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
 
     def laps_kv4_scatter(self, cu, start_pos, page_table, k_src, v_src, k4_pool, v4_pool, stream=None):
         """Quantises token-major bf16 K/V [n_tokens, n_kv_heads, head_dim] into 4-bit pools (new_kv4_pools)."""
-        n_seq, n_tok = self._expect_kv4(cu, {"start_pos": start_pos}, page_table, k4_pool, v4_pool), k_src.shape[0]
-        for what, t in (("k_src", k_src), ("v_src", v_src)):
-            _expect(what, t, torch.bfloat16, n_tok, self.cfg.n_kv_heads, self.cfg.head_dim)
-        self._guard_pools(k4_pool)
-        _after_current(stream)
-        _check(lib().laps_kv4_scatter(self._h, C.c_int32(n_seq), C.c_int32(n_tok), _p(cu), _p(start_pos), _p(page_table),
-                                      C.c_int32(page_table.shape[1]), _p(k_src), _p(v_src), _p(k4_pool), _p(v4_pool), _stream(stream)))
+        n_seq, width, (cu_p, start_p, table_p, k_p, v_p), device = self._kv4_call(cu, (("start_pos", start_pos),), page_table, k4_pool, v4_pool)
+        shape = (k_src.shape[0], self.cfg.n_kv_heads, self.cfg.head_dim)
+        src = _expect("k_src", k_src, torch.bfloat16, *shape), _expect("v_src", v_src, torch.bfloat16, *shape)
+        self._same_device(device, cu, start_pos, page_table, v4_pool, k_src, v_src)
+        s = self._kv4_stream(stream, k4_pool, device)
+        _check(lib().laps_kv4_scatter(self._h, n_seq, shape[0], cu_p, start_p, table_p, width, *src, k_p, v_p, s))
 
     def laps_kv4_gather(self, cu, start_pos, page_table, k4_pool, v4_pool, n_tokens, k_out=None, v_out=None, stream=None):
         """Reads token-major bf16 K/V back from 4-bit pools, into k_out / v_out if given.  Rows without a page keep what they
         held (nothing defined in tensors made here)."""
-        n_seq = self._expect_kv4(cu, {"start_pos": start_pos}, page_table, k4_pool, v4_pool)
-        shp = (n_tokens, self.cfg.n_kv_heads, self.cfg.head_dim)
-        outs = [torch.empty(shp, dtype=torch.bfloat16, device=k4_pool.device) if t is None else t for t in (k_out, v_out)]
-        for what, t in zip(("k_out", "v_out"), outs):
-            _expect(what, t, torch.bfloat16, *shp)
-        self._guard_pools(k4_pool)
-        _after_current(stream)
-        _check(lib().laps_kv4_gather(self._h, C.c_int32(n_seq), C.c_int32(n_tokens), _p(cu), _p(start_pos), _p(page_table),
-                                     C.c_int32(page_table.shape[1]), _p(k4_pool), _p(v4_pool), _p(outs[0]), _p(outs[1]), _stream(stream)))
-        _held_by(stream, *(t for t, given in zip(outs, (k_out, v_out)) if given is None))
+        n_seq, width, (cu_p, start_p, table_p, k_p, v_p), device = self._kv4_call(cu, (("start_pos", start_pos),), page_table, k4_pool, v4_pool)
+        shape = (n_tokens, self.cfg.n_kv_heads, self.cfg.head_dim)
+        made = [t is None for t in (k_out, v_out)]
+        outs = [torch.empty(shape, dtype=torch.bfloat16, device=k4_pool.device) if t is None else t for t in (k_out, v_out)]
+        dst = [_expect(what, t, torch.bfloat16, *shape) for what, t in zip(("k_out", "v_out"), outs)]
+        self._same_device(device, cu, start_pos, page_table, v4_pool, *outs)
+        s = self._kv4_stream(stream, k4_pool, device)
+        _check(lib().laps_kv4_gather(self._h, n_seq, n_tokens, cu_p, start_p, table_p, width, k_p, v_p, *dst, s))
+        _held_by(stream, *(t for t, m in zip(outs, made) if m))
         return outs[0], outs[1]
 
     def laps_attention_kv4_workspace_bytes(self, n_seq: int, n_tokens: int, max_pages: int) -> int:
-        return int(lib().laps_attention_kv4_workspace_bytes(self._h, C.c_int32(n_seq), C.c_int32(n_tokens), C.c_int32(max_pages)))
+        return lib().laps_attention_kv4_workspace_bytes(self._h, n_seq, n_tokens, max_pages)
 
     def laps_attention_kv4(self, cu, seq_len, prefix_len, page_table, k4_pool, v4_pool, q, out=None, stream=None):
         """laps_attention over 4-bit pools.  Rows of `out` that hold no token keep what they held (zeros if made here).  The
         workspace is this call's own: calls on several streams and captured graphs do not share one."""
-        n_seq = self._expect_kv4(cu, {"seq_len": seq_len, "prefix_len": prefix_len}, page_table, k4_pool, v4_pool)
-        n_tok, width = q.shape[0], self.cfg.n_q_heads * self.cfg.head_dim
-        _expect("q", q, torch.bfloat16, n_tok, width)
+        n_seq, width, (cu_p, len_p, pre_p, table_p, k_p, v_p), device = self._kv4_call(
+            cu, (("seq_len", seq_len), ("prefix_len", prefix_len)), page_table, k4_pool, v4_pool)
+        shape = (q.shape[0], self.cfg.n_q_heads * self.cfg.head_dim)
+        q_p = _expect("q", q, torch.bfloat16, *shape)
         made = out is None
         out = torch.zeros_like(q) if made else out
-        _expect("out", out, torch.bfloat16, n_tok, width)
-        need = self.laps_attention_kv4_workspace_bytes(n_seq, n_tok, page_table.shape[1])
+        out_p = _expect("out", out, torch.bfloat16, *shape)
+        self._same_device(device, cu, seq_len, prefix_len, page_table, v4_pool, q, out)
+        need = self.laps_attention_kv4_workspace_bytes(n_seq, shape[0], width)
         ws = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
-        self._guard_pools(k4_pool)
-        _after_current(stream)
-        _check(lib().laps_attention_kv4(self._h, C.c_int32(n_seq), C.c_int32(n_tok), _p(cu), _p(seq_len), _p(prefix_len),
-                                        _p(page_table), C.c_int32(page_table.shape[1]), _p(k4_pool), _p(v4_pool), _p(q), _p(out),
-                                        _p(ws), C.c_size_t(ws.numel()), _stream(stream)))
+        s = self._kv4_stream(stream, k4_pool, device)
+        _check(lib().laps_attention_kv4(self._h, n_seq, shape[0], cu_p, len_p, pre_p, table_p, width, k_p, v_p, q_p, out_p,
+                                        ws.data_ptr(), need, s))
         _held_by(stream, ws, *((out,) if made else ()))
         return out
 

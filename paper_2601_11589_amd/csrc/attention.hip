@@ -35,6 +35,7 @@
 // blocks of very different lengths.  Such launches run the 8-wave loop in a fixed number of workgroups, each of which walks
 // an equal share of the batch's (kv head, row block) units, worked out on the device from the batch's lengths; a unit cut
 // between shares leaves partial results like a split key range, merged in key order by a kernel of its own.
+#include "kv4.h"
 #include "laps_internal.h"
 
 #include <climits>
@@ -56,7 +57,8 @@ constexpr int MIN_TILES_PER_SPLIT = 4;   // key tiles per part of a split key ra
 // HALVES: the 4-wave loop forms its probabilities and row sums by half tiles, as the 8-wave loop does: the same bits.
 // PERSIST: a fixed number of workgroups, each walking its share of the batch (laps_dev_attn_bounds); a share may begin
 // and end inside a unit, whose parts then go through partial results like the splits.
-template <int HD, int NW, bool SPLIT, bool PERSIST, bool HALVES = false>
+// KV4: 4-bit pools (kv4.h).  Their codes travel as they are and become bf16 (exactly) on the way into LDS; all else is the same.
+template <int HD, int NW, bool SPLIT, bool PERSIST, bool HALVES = false, bool KV4 = false>
 __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const bf16_t* __restrict__ q, bf16_t* __restrict__ out,
                                                         float* __restrict__ part_o, float* __restrict__ part_ml,
                                                         const bf16_t* __restrict__ k_pool,
@@ -77,6 +79,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const bf16_t* __restri
 
     __shared__ __align__(16) u32x4 Ks[2][KT * CPR];   // double buffered: one barrier per tile
     __shared__ __align__(16) u32x4 Vs[2][HD * 8];
+    __shared__ int nan_first[KV4 ? NI : 1];   // first key whose V group is NaN, among those that not every row of the unit sees
 
     const int G = n_q / n_kv;
     // one unit: (item, kv head), key tiles [t0, t1) of it if PERSIST; slot: where a cut unit's result goes
@@ -138,8 +141,17 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const bf16_t* __restri
     // ---- tile copy assignment: chunk c = tid + i*NTHR of the tile's 4 pages.  All chunks a wave copies in one
     // pass lie in one page, so the page id is a wave-uniform (scalar) load.
     u32x4 kreg[NLD], vreg[NLD];   // landing registers of the tile copy
+    // KV4: a piece is 16 bytes of codes, 32 head_dim indices of a key or 8 of four keys, with its scales.  A tile has PIECES of K
+    // and of V; where there are threads for both, the upper half of them takes V's.
+    constexpr int PIECES = KT * HD / 32, PPP = HD / 2;   // in a tile, in a page
+    constexpr bool BOTH = PIECES == NTHR;
+    constexpr int NID = KV4 ? 1 : NLD;                   // page ids a thread needs for its share of a tile
+    const int piece = BOTH ? tid : tid % (NTHR / 2), in_page = piece % PPP;
+    const bool has_piece = piece < PIECES, takes_k = has_piece && (BOTH || tid < NTHR / 2), takes_v = has_piece && (BOTH || tid >= NTHR / 2);
+    [[maybe_unused]] unsigned kscale = 0, vscale = 0;
     auto page_id = [&](int j0, int i) -> int {
-        int pidx = j0 / LAPS_PAGE + __builtin_amdgcn_readfirstlane((tid + i * NTHR) / CPP);
+        const int in_tile = KV4 ? piece / PPP : (tid + i * NTHR) / CPP;
+        int pidx = j0 / LAPS_PAGE + (KV4 && HD == 64 ? in_tile : __builtin_amdgcn_readfirstlane(in_tile));
         pidx = pidx < n_pages_seq ? pidx : n_pages_seq - 1;  // past the end: any valid page, masked later
         return pt[pidx];
     };
@@ -149,7 +161,42 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const bf16_t* __restri
         const size_t page = (size_t)((pg > 0 && pg < n_pool_pages) ? pg : 0);
         return (page * n_kv + kvh) * CPP + within;
     };
+    auto load_k_of = [&](const int (&id)[NID]) {
+        if constexpr (KV4) {
+            if (!takes_k) return;
+            const size_t page = (size_t)((id[0] > 0 && id[0] < n_pool_pages) ? id[0] : 0);
+            const unsigned char* block = reinterpret_cast<const unsigned char*>(k_pool) + (page * n_kv + kvh) * kv4_block(HD);
+            kreg[0] = reinterpret_cast<const u32x4*>(block)[in_page];
+            kscale = block[kv4_codes(HD) + in_page];
+        } else {
+#pragma unroll
+            for (int i = 0; i < NLD; ++i) kreg[i] = reinterpret_cast<const u32x4*>(k_pool)[chunk_offset(id[i], i)];
+        }
+    };
+    auto load_v_of = [&](const int (&id)[NID]) {
+        if constexpr (KV4) {
+            if (!takes_v) return;
+            const size_t page = (size_t)((id[0] > 0 && id[0] < n_pool_pages) ? id[0] : 0);
+            const unsigned char* block = reinterpret_cast<const unsigned char*>(v_pool) + (page * n_kv + kvh) * kv4_block(HD);
+            vreg[0] = reinterpret_cast<const u32x4*>(block)[in_page];
+            vscale = reinterpret_cast<const unsigned*>(block + kv4_codes(HD))[in_page / 16 * 4 + in_page % 4];
+        } else {
+#pragma unroll
+            for (int i = 0; i < NLD; ++i) vreg[i] = reinterpret_cast<const u32x4*>(v_pool)[chunk_offset(id[i], i)];
+        }
+    };
     auto store_k = [&](int buf) {   // K page is [16 keys][HD]
+        if constexpr (KV4) {
+            if (!takes_k) return;
+            const int key = piece / (HD / 32), g = piece % (HD / 32);
+            const float sc = kv4_scale<0>(kscale);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int kc = 4 * g + c;
+                Ks[buf][key * CPR + (CPR == 16 ? swz16(key, kc) : swz8(key, kc))] = kv4_eight(kreg[0][c], sc);
+            }
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < NLD; ++i) {
             const int c = tid + i * NTHR;
@@ -159,6 +206,40 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const bf16_t* __restri
         }
     };
     auto store_v = [&](int j0, int buf) {   // V page is [HD][16 keys]: chunk = 8 consecutive keys of one head_dim index
+        if constexpr (KV4) {   // [HD / 8][16 keys][8 values]: four keys of eight head_dim indices
+            if (!takes_v) return;
+            const int c8 = in_page / 4, key = piece / PPP * LAPS_PAGE + in_page % 4 * 4;
+            u32x4 v = vreg[0];
+            unsigned sc = vscale;
+            if (j0 + KT - 1 > H + R0 / G) {   // some row of the unit does not see all of the tile's keys
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int k = j0 + key + e;
+                    const bool past = k >= kv_len, is_nan = ((sc >> (8 * e)) & 255u) == 255u;
+                    if (past || is_nan) {   // weight zero times either must stay zero; rows that see a NaN get it at the end
+                        if (!past) atomicMin(&nan_first[c8 / 4], k);
+                        v[e] = 0u;
+                        sc &= ~(255u << (8 * e));
+                    }
+                }
+            }
+            auto row_pair = [&](auto B) {
+                constexpr int b = decltype(B)::value;
+                const unsigned w0 = kv4_pair<b>(v.x, kv4_scale<0>(sc)), w1 = kv4_pair<b>(v.y, kv4_scale<1>(sc));
+                const unsigned w2 = kv4_pair<b>(v.z, kv4_scale<2>(sc)), w3 = kv4_pair<b>(v.w, kv4_scale<3>(sc));
+                const u32x2 even = {__builtin_amdgcn_perm(w1, w0, 0x05040100u), __builtin_amdgcn_perm(w3, w2, 0x05040100u)};
+                const u32x2 odd = {__builtin_amdgcn_perm(w1, w0, 0x07060302u), __builtin_amdgcn_perm(w3, w2, 0x07060302u)};
+                const int row = 8 * c8 + 2 * b;
+                u32x2* dst = reinterpret_cast<u32x2*>(Vs[buf]);
+                dst[(row * 8 + swz8(row, key / 8)) * 2 + (key / 4 & 1)] = even;
+                dst[((row + 1) * 8 + swz8(row + 1, key / 8)) * 2 + (key / 4 & 1)] = odd;
+            };
+            row_pair(std::integral_constant<int, 0>{});
+            row_pair(std::integral_constant<int, 1>{});
+            row_pair(std::integral_constant<int, 2>{});
+            row_pair(std::integral_constant<int, 3>{});
+            return;
+        }
         const bool tail = (j0 + KT > kv_len);
 #pragma unroll
         for (int i = 0; i < NLD; ++i) {
@@ -336,6 +417,11 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const bf16_t* __restri
     };
 
     const auto exists = [&](int j) { return j < kv_end; };
+    if constexpr (KV4) {   // before the first store of V, after the last look of the unit before
+        if (PERSIST) __syncthreads();
+        if (tid < NI) nan_first[tid] = INT_MAX;
+        __syncthreads();
+    }
     if constexpr (NW == 8) {
         // Long prompts.  The loop is software-pipelined three deep over 32-key half tiles: in step w the matrix
         // cores form the scores of half tile w + 1 and add half tile w - 1 to O while the vector ALU turns the scores
@@ -347,19 +433,13 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const bf16_t* __restri
         //   2t + 1: scores of (t+1, keys 0..31), softmax of (t, keys 32..63), O += (t, keys 0..31)
         // and there is one tile step more than tiles (its first half adds the last half tile to O).
         // page ids (scalars) are fetched one tile step before the loads that use them
-        int idk[NLD], idv[NLD];
+        int idk[NID], idv[NID];
         auto fetch_ids = [&](int jk, int jv) {
 #pragma unroll
-            for (int i = 0; i < NLD; ++i) idk[i] = page_id(jk, i), idv[i] = page_id(jv, i);
+            for (int i = 0; i < NID; ++i) idk[i] = page_id(jk, i), idv[i] = page_id(jv, i);
         };
-        auto load_k = [&]() {
-#pragma unroll
-            for (int i = 0; i < NLD; ++i) kreg[i] = reinterpret_cast<const u32x4*>(k_pool)[chunk_offset(idk[i], i)];
-        };
-        auto load_v = [&]() {
-#pragma unroll
-            for (int i = 0; i < NLD; ++i) vreg[i] = reinterpret_cast<const u32x4*>(v_pool)[chunk_offset(idv[i], i)];
-        };
+        auto load_k = [&]() { load_k_of(idk); };
+        auto load_v = [&]() { load_v_of(idv); };
         // wave-uniform: half tile (tile at key j, half h) exists and some row of this wave sees one of its keys
         const auto visible = [&](int j, int h) { return j >= kv_begin && j < kv_end && j + 32 * h <= vis_max; };
         constexpr int NQ = KSTEPS;       // matrix instructions of each product per half tile (equal: HD / 16)
@@ -486,14 +566,19 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const bf16_t* __restri
         // Short prompts and key-range splits: a few tiles per workgroup, latency matters more than overlap.  The
         // page ids of a tile are fetched one step before its data, so that the two dependent loads (table entry,
         // then the page itself) do not add up on the critical path of every tile.
-        int pgn[NLD];
+        int pgn[NID];
         auto load_pages = [&](int j0) {
 #pragma unroll
-            for (int i = 0; i < NLD; ++i) pgn[i] = page_id(j0, i);
+            for (int i = 0; i < NID; ++i) pgn[i] = page_id(j0, i);
         };
         auto load_tile = [&]() {   // uses the ids load_pages fetched
+            if constexpr (KV4) {
+                load_k_of(pgn);
+                load_v_of(pgn);
+                return;
+            }
 #pragma unroll
-            for (int i = 0; i < NLD; ++i) {
+            for (int i = 0; i < NID; ++i) {
                 const size_t off = chunk_offset(pgn[i], i);
                 kreg[i] = reinterpret_cast<const u32x4*>(k_pool)[off];
                 vreg[i] = reinterpret_cast<const u32x4*>(v_pool)[off];
@@ -542,6 +627,16 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const bf16_t* __restri
             }
             __syncthreads();
         }
+    }
+
+    if constexpr (KV4) {
+        __syncthreads();   // V of the last tile is stored
+#pragma unroll
+        for (int ni = 0; ni < NI; ++ni)
+            if (nan_first[ni] <= limit) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[ni][i] = __builtin_nanf("");
+            }
     }
 
     // ---- normalise and store: lane owns row r; register i of sub-tile ni is head_dim index
@@ -740,26 +835,26 @@ __global__ __launch_bounds__(128 * MERGE_GROUPS) void attn_merge_kernel(
     }
 }
 
-template <int HD, int NW, bool HALVES = false>
+template <int HD, int NW, bool HALVES, bool KV4>
 int launch_attn(const bf16_t* q, bf16_t* out, const bf16_t* k_pool, const bf16_t* v_pool, const int4* desc,
                 const int* page_table, int max_pages, const int* tile_start, int n_seq, int max_items, int n_q, int n_kv, int n_pool_pages, int n_tokens,
                 hipStream_t s) {
     const float scale_log2e = 1.4426950408889634f / sqrtf((float)HD);
-    hipLaunchKernelGGL((attn_kernel<HD, NW, false, false, HALVES>), dim3(max_items, n_kv), dim3(NW * 64), 0, s, q, out, nullptr,
+    hipLaunchKernelGGL((attn_kernel<HD, NW, false, false, HALVES, KV4>), dim3(max_items, n_kv), dim3(NW * 64), 0, s, q, out, nullptr,
                        nullptr, k_pool, v_pool, desc, page_table, max_pages, tile_start,
                        n_seq, n_q, n_kv, scale_log2e, n_pool_pages, n_tokens, max_items, nullptr);
     LAPS_LAUNCH_CHECK();
     return LAPS_OK;
 }
 
-template <int HD>
+template <int HD, bool KV4>
 int launch_attn_persistent(const bf16_t* q, bf16_t* out, float* part, int n_wgs, const int4* bounds, const bf16_t* k_pool,
                            const bf16_t* v_pool, const int4* desc,
                            const int* page_table, int max_pages, const int* tile_start, int n_seq,
                            int max_items, int n_q, int n_kv, int n_pool_pages, int n_tokens, hipStream_t s) {
     const float scale_log2e = 1.4426950408889634f / sqrtf((float)HD);
     float* part_ml = part + (size_t)2 * n_wgs * LAPS_ATTN_LONG_ROWS * HD;
-    hipLaunchKernelGGL((attn_kernel<HD, 8, false, true>), dim3(n_wgs), dim3(512), 0, s, q, out, part, part_ml, k_pool, v_pool,
+    hipLaunchKernelGGL((attn_kernel<HD, 8, false, true, false, KV4>), dim3(n_wgs), dim3(512), 0, s, q, out, part, part_ml, k_pool, v_pool,
                        desc, page_table, max_pages, tile_start, n_seq, n_q, n_kv,
                        scale_log2e, n_pool_pages, n_tokens, max_items, bounds);
     LAPS_LAUNCH_CHECK();
@@ -769,7 +864,7 @@ int launch_attn_persistent(const bf16_t* q, bf16_t* out, float* part, int n_wgs,
     return LAPS_OK;
 }
 
-template <int HD>
+template <int HD, bool KV4>
 int launch_attn_split(const bf16_t* q, bf16_t* out, float* part, const bf16_t* k_pool, const bf16_t* v_pool,
                       const int4* desc, const int* page_table,
                       int max_pages, const int* tile_start, int n_seq, int max_items, int n_split,
@@ -778,7 +873,7 @@ int launch_attn_split(const bf16_t* q, bf16_t* out, float* part, const bf16_t* k
     const size_t blocks = (size_t)max_items * n_kv * n_split;
     float* part_o = part;
     float* part_ml = part + blocks * 128 * HD;
-    hipLaunchKernelGGL((attn_kernel<HD, 4, true, false>), dim3(max_items, n_kv, n_split), dim3(256), 0, s, q, out, part_o, part_ml,
+    hipLaunchKernelGGL((attn_kernel<HD, 4, true, false, false, KV4>), dim3(max_items, n_kv, n_split), dim3(256), 0, s, q, out, part_o, part_ml,
                        k_pool, v_pool, desc, page_table, max_pages, tile_start, n_seq,
                        n_q, n_kv, scale_log2e, n_pool_pages, n_tokens, max_items, nullptr);
     LAPS_LAUNCH_CHECK();
@@ -801,6 +896,10 @@ static constexpr int kSplitTargetBlocks = 512;   // aim for two workgroups per c
 static constexpr int kSplitBelowBlocks = 256;    // launches with fewer un-split workgroups than this are split
 static constexpr int kSplitMax = 64;
 
+size_t laps_attn_partial_want(int n_seq, int n_tokens, int group, int n_kv, int hd, int max_pages) {
+    const size_t shares = (size_t)2 * LAPS_ATTN_MAX_WGS * LAPS_ATTN_LONG_ROWS * (hd + 2) * sizeof(float), parts = laps_attn_partial_bytes(hd, max_pages);
+    return laps_attn_persistent_wgs(n_seq, n_tokens, group, n_kv, hd, max_pages, shares) > 0 && shares > parts ? shares : parts;
+}
 size_t laps_attn_partial_bytes(int hd, int max_pages) {
     // page tables too narrow for two splits never take the split path (same test as attn_blocking)
     if (((long)max_pages * LAPS_PAGE + KT - 1) / KT < 2 * MIN_TILES_PER_SPLIT) return 0;
@@ -915,43 +1014,45 @@ int laps_attn_persistent_wgs(int n_seq, int n_tokens, int group, int n_kv, int h
     return wgs;
 }
 
-int laps_launch_attention(const bf16_t* q, bf16_t* out, const bf16_t* k_pool, const bf16_t* v_pool,
-                          const int* page_table, int max_pages, int n_seq, int n_tokens, const int* tile_start,
-                          const int* item_seq, float* partial, size_t partial_bytes, int n_q, int n_kv, int hd, int n_pool_pages,
-                          hipStream_t s) {
+template <int HD, bool KV4>
+static int launch_attention(const bf16_t* q, bf16_t* out, const bf16_t* k_pool, const bf16_t* v_pool, const int* page_table, int max_pages,
+                            int n_seq, int n_tokens, const int* tile_start, const int* item_seq, float* partial, size_t partial_bytes,
+                            int n_q, int n_kv, int n_pool_pages, hipStream_t s) {
     int mt, max_items, n_split, min_tiles;
     attn_blocking(n_seq, n_tokens, n_q / n_kv, n_kv, max_pages, &mt, &max_items, &n_split, &min_tiles);
-    const int n_wgs = partial ? laps_attn_persistent_wgs(n_seq, n_tokens, n_q / n_kv, n_kv, hd, max_pages, partial_bytes) : 0;
+    const int n_wgs = partial ? laps_attn_persistent_wgs(n_seq, n_tokens, n_q / n_kv, n_kv, HD, max_pages, partial_bytes) : 0;
     int* pre;
     int4 *bounds, *desc;
     laps_attn_item_tables(const_cast<int*>(item_seq), n_tokens, n_seq, n_q / n_kv, &pre, &bounds, &desc);
-    if (n_wgs > 0) {
-        auto launch = hd == 128 ? launch_attn_persistent<128> : launch_attn_persistent<64>;
-        return launch(q, out, partial, n_wgs, bounds, k_pool, v_pool, desc, page_table, max_pages,
-                      tile_start, n_seq, max_items, n_q, n_kv, n_pool_pages, n_tokens, s);
-    }
+    if (n_wgs > 0)
+        return launch_attn_persistent<HD, KV4>(q, out, partial, n_wgs, bounds, k_pool, v_pool, desc, page_table, max_pages, tile_start,
+                                               n_seq, max_items, n_q, n_kv, n_pool_pages, n_tokens, s);
     if (n_split > 1) {
         if (!partial) {
             laps_set_error("attention: key-split launch needs the partial-result workspace");
             return LAPS_EINVAL;
         }
-        if (hd == 128) return launch_attn_split<128>(q, out, partial, k_pool, v_pool, desc, page_table, max_pages, tile_start, n_seq, max_items, n_split, n_q, n_kv, n_pool_pages, n_tokens, s);
-        if (hd == 64) return launch_attn_split<64>(q, out, partial, k_pool, v_pool, desc, page_table, max_pages, tile_start, n_seq, max_items, n_split, n_q, n_kv, n_pool_pages, n_tokens, s);
+        return launch_attn_split<HD, KV4>(q, out, partial, k_pool, v_pool, desc, page_table, max_pages, tile_start, n_seq, max_items, n_split,
+                                          n_q, n_kv, n_pool_pages, n_tokens, s);
     }
     // 128-row blocks that would be 256-row ones over more key tiles: summed up as those do, so that the width of the page table
     // does not show in the result (the sums of rounded probabilities are also the ones that match the second product:
     // 32B prompts of 64 tokens 1.79e-3 from 64 bits, with sums of unrounded ones 1.81e-3; the same time)
     const bool halves = (long)n_tokens * (n_q / n_kv) > 128L * n_seq;
-    if (hd == 128) {
-        if (mt == 2) return launch_attn<128, 8>(q, out, k_pool, v_pool, desc, page_table, max_pages, tile_start, n_seq, max_items, n_q, n_kv, n_pool_pages, n_tokens, s);
-        if (halves) return launch_attn<128, 4, true>(q, out, k_pool, v_pool, desc, page_table, max_pages, tile_start, n_seq, max_items, n_q, n_kv, n_pool_pages, n_tokens, s);
-        return launch_attn<128, 4>(q, out, k_pool, v_pool, desc, page_table, max_pages, tile_start, n_seq, max_items, n_q, n_kv, n_pool_pages, n_tokens, s);
+    auto launch = mt == 2 ? launch_attn<HD, 8, false, KV4> : halves ? launch_attn<HD, 4, true, KV4> : launch_attn<HD, 4, false, KV4>;
+    return launch(q, out, k_pool, v_pool, desc, page_table, max_pages, tile_start, n_seq, max_items, n_q, n_kv, n_pool_pages, n_tokens, s);
+}
+
+int laps_launch_attention(const bf16_t* q, bf16_t* out, const void* k_pool, const void* v_pool, bool kv4,
+                          const int* page_table, int max_pages, int n_seq, int n_tokens, const int* tile_start,
+                          const int* item_seq, float* partial, size_t partial_bytes, int n_q, int n_kv, int hd, int n_pool_pages,
+                          hipStream_t s) {
+    if (hd != 64 && hd != 128) {
+        laps_set_error("attention: head_dim %d not supported (64 or 128)", hd);
+        return LAPS_EINVAL;
     }
-    if (hd == 64) {
-        if (mt == 2) return launch_attn<64, 8>(q, out, k_pool, v_pool, desc, page_table, max_pages, tile_start, n_seq, max_items, n_q, n_kv, n_pool_pages, n_tokens, s);
-        if (halves) return launch_attn<64, 4, true>(q, out, k_pool, v_pool, desc, page_table, max_pages, tile_start, n_seq, max_items, n_q, n_kv, n_pool_pages, n_tokens, s);
-        return launch_attn<64, 4>(q, out, k_pool, v_pool, desc, page_table, max_pages, tile_start, n_seq, max_items, n_q, n_kv, n_pool_pages, n_tokens, s);
-    }
-    laps_set_error("attention: head_dim %d not supported (64 or 128)", hd);
-    return LAPS_EINVAL;
+    auto launch = hd == 128 ? (kv4 ? launch_attention<128, true> : launch_attention<128, false>)
+                            : (kv4 ? launch_attention<64, true> : launch_attention<64, false>);
+    return launch(q, out, static_cast<const bf16_t*>(k_pool), static_cast<const bf16_t*>(v_pool), page_table, max_pages, n_seq, n_tokens,
+                  tile_start, item_seq, partial, partial_bytes, n_q, n_kv, n_pool_pages, s);
 }

@@ -359,6 +359,13 @@ int launch_rows(const Kv4Attn& a, const Kv4RowsPlan& p, float* part, hipStream_t
 
 }  // namespace
 
+// Blocks of 128 rows read and unpack the keys once for all of them, but pay for 128 whatever they hold, and for their work-item
+// table.  This kernel against blocks, graph replays, us: 32B, 16 sequences over 2048 keys, 4 / 6 / 8 / 16 tokens each 29 / 32 / 43 / 63
+// and 36 / 37 / 42 / 42; one over 4000 keys, 1 / 8 / 16 tokens 9.6 / 16.4 / 22.7 and 16.8 / 17.6 / 18.5.
+bool laps_kv4_takes_rows(int n_seq, int n_tokens, int n_q, int n_kv) {
+    return (long)n_tokens * (n_q / n_kv) <= 32L * n_seq;
+}
+
 Kv4RowsPlan laps_kv4_rows_plan(int n_seq, int n_tokens, int n_q, int n_kv, int max_pages) {
     const long rows = (long)n_tokens * (n_q / n_kv);
     long blocks = (rows + 16L * n_seq - 1) / (16L * n_seq);

@@ -385,7 +385,7 @@ static int run_layers(laps_ctx* c, const laps_layer_weights* w, int n_layers, co
         }
         {
             ProfScope ps(c, s, LAPS_K_ATTN, capturing);
-            LAPS_TRY(laps_launch_attention(q, attn, kp, vp, b.page_table, b.max_pages, b.n_seq, M, tile_start, item_seq,
+            LAPS_TRY(laps_launch_attention(q, attn, kp, vp, false, b.page_table, b.max_pages, b.n_seq, M, tile_start, item_seq,
                                            partial, partial_bytes, cf.n_q_heads, cf.n_kv_heads, hd, c->pool_pages, s));
         }
         // x_mid = resid + attn W_o^T ; r = rmsnorm(x_mid; ln2)
@@ -619,11 +619,24 @@ extern "C" int laps_kv4_gather(laps_ctx* c, int32_t n_seq, int32_t n_tokens, con
                     const_cast<void*>(v_pool), stream);
 }
 
+// Workspace of the block kernels: lengths, work items, partial results.
+static WsLayout kv4_layout(const laps_model_cfg& c, int n_seq, int n_tokens, int max_pages) {
+    WsLayout w = {};
+    const int group = c.n_q_heads / c.n_kv_heads;
+    w.tile_start = align256((size_t)n_seq * 4);
+    w.item_seq = w.tile_start + align256((size_t)(n_seq + 1) * 4);
+    w.partial = w.item_seq + align256(laps_attn_item_table_bytes(n_tokens, n_seq, group));
+    w.total = w.partial + align256(laps_attn_partial_want(n_seq, n_tokens, group, c.n_kv_heads, c.head_dim, max_pages));
+    return w;
+}
+
 extern "C" size_t laps_attention_kv4_workspace_bytes(const laps_ctx* c, int32_t n_seq, int32_t n_tokens, int32_t max_pages) {
     if (!c || n_seq < 1 || n_tokens < 1 || max_pages < 1 || max_pages > LAPS_KV4_MAX_PAGES || (long)n_seq * c->cfg.n_q_heads > LAPS_KV4_MAX_SEQ_HEADS)
         return 0;
-    const Kv4RowsPlan p = laps_kv4_rows_plan(n_seq, n_tokens, c->cfg.n_q_heads, c->cfg.n_kv_heads, max_pages);
-    return align256(laps_kv4_rows_bytes(p, n_tokens, c->cfg.n_q_heads, c->cfg.head_dim) + 1);
+    const laps_model_cfg& cf = c->cfg;
+    if (!laps_kv4_takes_rows(n_seq, n_tokens, cf.n_q_heads, cf.n_kv_heads)) return kv4_layout(cf, n_seq, n_tokens, max_pages).total;
+    const Kv4RowsPlan p = laps_kv4_rows_plan(n_seq, n_tokens, cf.n_q_heads, cf.n_kv_heads, max_pages);
+    return align256(laps_kv4_rows_bytes(p, n_tokens, cf.n_q_heads, cf.head_dim) + 1);
 }
 
 extern "C" int laps_attention_kv4(laps_ctx* c, int32_t n_seq, int32_t n_tokens, const int32_t* cu, const int32_t* seq_len,
@@ -648,11 +661,23 @@ extern "C" int laps_attention_kv4(laps_ctx* c, int32_t n_seq, int32_t n_tokens, 
         laps_set_error("attention_kv4: workspace too small (%zu < %zu bytes)", ws_bytes, need);
         return LAPS_ENOMEM;
     }
-    const Kv4Attn a = {static_cast<const bf16_t*>(q), static_cast<bf16_t*>(out), static_cast<const unsigned char*>(k_pool),
-                       static_cast<const unsigned char*>(v_pool), cu, seq_len, prefix_len, pt, n_seq, n_tokens, max_pages,
-                       c->pool_pages, c->cfg.n_q_heads, c->cfg.n_kv_heads, c->cfg.head_dim};
-    const Kv4RowsPlan p = laps_kv4_rows_plan(n_seq, n_tokens, a.n_q, a.n_kv, max_pages);
-    return laps_launch_kv4_rows(a, p, p.parts > 1 ? static_cast<float*>(ws) : nullptr, static_cast<hipStream_t>(stream));
+    const laps_model_cfg& cf = c->cfg;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (laps_kv4_takes_rows(n_seq, n_tokens, cf.n_q_heads, cf.n_kv_heads)) {
+        const Kv4Attn a = {static_cast<const bf16_t*>(q), static_cast<bf16_t*>(out), static_cast<const unsigned char*>(k_pool),
+                           static_cast<const unsigned char*>(v_pool), cu, seq_len, prefix_len, pt, n_seq, n_tokens, max_pages,
+                           c->pool_pages, cf.n_q_heads, cf.n_kv_heads, cf.head_dim};
+        const Kv4RowsPlan p = laps_kv4_rows_plan(n_seq, n_tokens, a.n_q, a.n_kv, max_pages);
+        return laps_launch_kv4_rows(a, p, p.parts > 1 ? static_cast<float*>(ws) : nullptr, s);
+    }
+    const WsLayout L = kv4_layout(cf, n_seq, n_tokens, max_pages);
+    unsigned char* w8 = static_cast<unsigned char*>(ws);
+    const BatchDesc b{n_seq, n_tokens, cu, seq_len, prefix_len, pt, max_pages};
+    LAPS_TRY(laps_launch_begin(begin_args(c, b, w8, L), s));
+    return laps_launch_attention(static_cast<const bf16_t*>(q), static_cast<bf16_t*>(out), k_pool, v_pool, true, pt, max_pages, n_seq,
+                                 n_tokens, reinterpret_cast<int*>(w8 + L.tile_start), reinterpret_cast<int*>(w8 + L.item_seq),
+                                 reinterpret_cast<float*>(w8 + L.partial), L.total - L.partial, cf.n_q_heads, cf.n_kv_heads,
+                                 cf.head_dim, c->pool_pages, s);
 }
 
 extern "C" size_t laps_gemm_workspace_bytes(int32_t m, int32_t n, int32_t k, int32_t split_k) {
@@ -757,7 +782,7 @@ extern "C" int laps_attention(laps_ctx* c, int32_t n_seq, int32_t n_tokens, cons
     LAPS_TRY(laps_launch_begin(begin_args(c, b, w8, L), s));
     const size_t partial_bytes = L.total - L.partial;
     return laps_launch_attention(static_cast<const bf16_t*>(q), static_cast<bf16_t*>(out),
-                                 static_cast<const bf16_t*>(k_pool), static_cast<const bf16_t*>(v_pool), pt, max_pages, n_seq, n_tokens,
+                                 k_pool, v_pool, false, pt, max_pages, n_seq, n_tokens,
                                  reinterpret_cast<int*>(w8 + L.tile_start), reinterpret_cast<int*>(w8 + L.item_seq),
                                  reinterpret_cast<float*>(w8 + L.partial), partial_bytes, c->cfg.n_q_heads, c->cfg.n_kv_heads, c->cfg.head_dim, c->pool_pages, s);
 }

@@ -73,6 +73,8 @@ struct Kv4RowsPlan {
     int row_blocks;   // blocks of rows that workgroups of their own walk, a sequence and kv head
     int parts;        // most parts of a sequence's keys
 };
+// Which of the two kernels a launch shape takes: this one, or the blocks of 128 or 256 rows of the bf16 pools' attention.
+bool laps_kv4_takes_rows(int n_seq, int n_tokens, int n_q, int n_kv);
 Kv4RowsPlan laps_kv4_rows_plan(int n_seq, int n_tokens, int n_q, int n_kv, int max_pages);
 size_t laps_kv4_rows_bytes(const Kv4RowsPlan& p, int n_tokens, int n_q, int hd);   // partial results of the parts
 int laps_launch_kv4_rows(const Kv4Attn& a, const Kv4RowsPlan& p, float* partial, hipStream_t s);

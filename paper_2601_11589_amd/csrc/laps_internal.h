@@ -312,6 +312,8 @@ static __device__ __forceinline__ void laps_dev_attn_bounds(const int* __restric
 // calls for splitting the key range; it may be NULL only if max_pages * 16 < 512.  partial_bytes must be that of the table's shares.
 // tile_start: n_seq + 1 ints; item_seq: laps_attn_item_table_bytes (sequence of every row-block work item).
 size_t laps_attn_partial_bytes(int hd, int max_pages);   // 0 when page tables this narrow never split
+// For a launch of its own: as much as it can use.
+size_t laps_attn_partial_want(int n_seq, int n_tokens, int group, int n_kv, int hd, int max_pages);
 // Work-item table: item_seq, then the cost prefix sums and the bounds of the persistent kernel and the items' descriptions.
 size_t laps_attn_item_table_bytes(int max_tokens, int max_seqs, int group);
 void laps_attn_item_tables(int* item_seq, int n_tokens, int n_seq, int group, int** pre, int4** bounds, int4** desc);
@@ -323,7 +325,8 @@ int laps_attn_persistent_wgs(int n_seq, int n_tokens, int group, int n_kv, int h
 void laps_attn_plan(int n_seq, int n_tokens, int group, int n_kv, int max_pages, int* rows_per_wg, int* max_items,
                     int* n_split, int* min_tiles_per_split);
 // Lengths and row offsets are those that the kernel which began or staged the batch has put into the table.
-int laps_launch_attention(const bf16_t* q, bf16_t* out, const bf16_t* k_pool, const bf16_t* v_pool,
+// kv4: 4-bit pools.
+int laps_launch_attention(const bf16_t* q, bf16_t* out, const void* k_pool, const void* v_pool, bool kv4,
                           const int* page_table, int max_pages, int n_seq, int n_tokens, const int* tile_start,
                           const int* item_seq, float* partial, size_t partial_bytes, int n_q, int n_kv, int hd, int n_pool_pages,
                           hipStream_t s);
