@@ -45,10 +45,16 @@ __device__ __forceinline__ bool seq_range(int seq, const int* cu, const int* seq
     return true;
 }
 
-// Parts of a sequence's keys: of equal length, at least one step a wave each.
-__device__ __forceinline__ int part_steps(int kv_len, int parts, int* used) {
-    const int steps = (kv_len + STEP - 1) / STEP, rounds = (steps + WAVES - 1) / WAVES;
-    const int n = rounds < parts ? rounds : parts, each = (rounds + n - 1) / n;
+// Parts of a sequence's keys, all of equal length: a share of `parts` of the longest range that the page table holds, but at least
+// min_parts of them as far as there is a step for every wave.
+__device__ __forceinline__ int part_steps(int kv_len, int max_pages, int parts, int min_parts, int* used) {
+    const int rounds = (kv_len + STEP * WAVES - 1) / (STEP * WAVES), most = (max_pages + 2 * WAVES - 1) / (2 * WAVES);
+    const int share = (most + parts - 1) / parts;
+    int n = (rounds + share - 1) / share;
+    n = n < min_parts ? min_parts : n;
+    n = n < parts ? n : parts;
+    n = n < rounds ? n : rounds;
+    const int each = (rounds + n - 1) / n;
     *used = (rounds + each - 1) / each;
     return each * WAVES;
 }
@@ -56,51 +62,64 @@ __device__ __forceinline__ int part_steps(int kv_len, int parts, int* used) {
 // One step's codes and scales as they come from the pools.
 template <int HD>
 struct Piece {
-    unsigned k[2][HD / 32], ks[2];   // [page]: HD / 4 codes of key i, their group's scale byte
+    unsigned k[2][HD / 32], ks[2];   // [page]: HD / 4 codes of key i, the dword with their group's scale byte
     u32x4 v[2];                      // eight codes (HD 64: four of them used) of keys 4g .. 4g + 3
     unsigned vs[2];                  // those keys' scale bytes
 };
 
-template <int HD>
-__global__ __launch_bounds__(WAVES * 64) void attn_rows_kernel(
+// NR: blocks of 16 rows that share what is read and unpacked.
+template <int HD, int NR>
+__global__ __launch_bounds__(WAVES * 64, NR == 1 ? 3 : 2) void attn_rows_kernel(
     const bf16_t* __restrict__ q, bf16_t* __restrict__ out, const byte_t* __restrict__ k_pool, const byte_t* __restrict__ v_pool,
     const int* __restrict__ cu, const int* __restrict__ seq_len, const int* __restrict__ prefix_len,
-    const int* __restrict__ page_table, int max_pages, int n_tokens, int n_q, int n_kv, int n_pool_pages, int row_blocks, int parts,
-    float scale_log2e, float* __restrict__ part_o, float* __restrict__ part_ml) {
+    const int* __restrict__ page_table, int max_pages, int n_seq, int n_tokens, int n_q, int n_kv, int n_pool_pages, int row_blocks, int parts,
+    int min_parts, float scale_log2e, float* __restrict__ part_o, float* __restrict__ part_ml) {
     constexpr int KS = HD / 32;        // matrix instructions of a page's scores
     constexpr int DL = HD / 16;        // head_dim indices of a lane of V, and of the result's 16 rows each
-    constexpr int BLOCK = kv4_block(HD), CODES = kv4_codes(HD);
+    constexpr int BLOCK = kv4_block(HD), CODES = kv4_codes(HD), ROWS = 16 * NR;
     __shared__ __align__(16) float red_o[WAVES][16][HD + 4];
     __shared__ float red_ml[WAVES][2][16];
 
-    const int G = n_q / n_kv, kvh = blockIdx.x % n_kv, rest = blockIdx.x / n_kv, rb0 = rest % row_blocks, seq = rest / row_blocks, part = blockIdx.y;
+    // Workgroup b runs on XCD b % 8.  The kv heads of a (sequence, part, row block) go to one XCD side by side: a page's heads are
+    // neighbours in memory and a block is 8.5 (4.25) lines of 128 bytes, so that each fetches a line that the next one needs too.
+    const int G = n_q / n_kv, kvh = blockIdx.x / 8 % n_kv, rest = blockIdx.x / 8 / n_kv * 8 + blockIdx.x % 8;
+    const int rb0 = rest % row_blocks, part = rest / row_blocks % parts, seq = rest / row_blocks / parts;
+    if (seq >= n_seq) return;
     SeqRange r;
     if (!seq_range(seq, cu, seq_len, prefix_len, n_tokens, max_pages, &r)) return;
     const int n_rows = r.L * G, kv_len = r.H + r.L;
     int used;
-    const int each = part_steps(kv_len, parts, &used);
+    const int each = part_steps(kv_len, max_pages, parts, min_parts, &used);
     if (part >= used) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4;
     const int need = (kv_len + LAPS_PAGE - 1) / LAPS_PAGE, n_pages = need < max_pages ? need : max_pages;
     const int* pt = page_table + (size_t)seq * max_pages;
+    const unsigned k_turn = (8 * (HD == 128 ? g : 2 * (i & 1) + (g >> 1)) + 9) & 31;   // right rotation that brings the lane's scale byte up
     const int v_chunk = HD == 128 ? i : i >> 1, v_group = i / (KV4_GROUP / DL), o_group = g * 4 * DL / KV4_GROUP;
 
-    for (int rb = rb0; rb * 16 < n_rows; rb += row_blocks) {
-        const int row = rb * 16 + i, rc = row < n_rows ? row : n_rows - 1, tq = rc / G;
-        const int limit = r.H + tq;                                            // last key this lane's row sees
-        const int last_row = rb * 16 + 15 < n_rows ? rb * 16 + 15 : n_rows - 1;
-        const int vis_min = r.H + rb * 16 / G, kv_end = r.H + last_row / G + 1;  // seen by every row, by the last row
-        bf16x8 qf[KS];
-        {
+    for (int rb = rb0; rb * ROWS < n_rows; rb += row_blocks) {
+        const int last_row = rb * ROWS + ROWS - 1 < n_rows ? rb * ROWS + ROWS - 1 : n_rows - 1;
+        const int vis_min = r.H + rb * ROWS / G, kv_end = r.H + last_row / G + 1;  // seen by every row, by the last row
+        int limit[NR];                                                             // last key this lane's rows see
+        bf16x8 qf[NR][KS];
+#pragma unroll
+        for (int a = 0; a < NR; ++a) {
+            const int row = rb * ROWS + 16 * a + i, rc = row < n_rows ? row : n_rows - 1, tq = rc / G;
+            limit[a] = r.H + tq;
             const u32x4* qp = reinterpret_cast<const u32x4*>(q + (size_t)(r.rs + tq) * n_q * HD + (size_t)(kvh * G + rc - tq * G) * HD);
 #pragma unroll
-            for (int kk = 0; kk < KS; ++kk) qf[kk] = __builtin_bit_cast(bf16x8, qp[g * KS + kk]);
+            for (int kk = 0; kk < KS; ++kk) qf[a][kk] = __builtin_bit_cast(bf16x8, qp[g * KS + kk]);
         }
-        f32x4 o[DL];
+        f32x4 o[NR][DL];
+        float m_run[NR], l_run[NR];   // reference in log2 units (the same in the four lanes of a row), this lane's sum
 #pragma unroll
-        for (int j = 0; j < DL; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        float m_run = -INFINITY, l_run = 0.f;   // reference in log2 units (the same in the four lanes of a row), this lane's sum
-        int nan_key = INT_MAX;                  // first key with a NaN group in this lane's V_group, where not every row sees it
+        for (int a = 0; a < NR; ++a) {
+            m_run[a] = -INFINITY;
+            l_run[a] = 0.f;
+#pragma unroll
+            for (int j = 0; j < DL; ++j) o[a][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        int nan_key = INT_MAX;        // first key with a NaN group in this lane's v_group, where not every row sees it
 
         const int s_begin = part * each + wave;
         int s_end = (kv_end + STEP - 1) / STEP;
@@ -113,6 +132,7 @@ __global__ __launch_bounds__(WAVES * 64) void attn_rows_kernel(
             p = p < n_pages ? p : n_pages - 1;                 // past the end: any page, masked below
             const int id = pt[p];
             ids = (id > 0 && id < n_pool_pages) ? id : 0;      // unset, or not a page of the pool
+            asm volatile("" : "+v"(ids));   // waited for here: behind the join it would be waited for at every step, with all loads in flight
         };
         auto load = [&](int n, Piece<HD>& x) {
             if ((n & 31) == 0) fetch_ids(n);
@@ -125,27 +145,30 @@ __global__ __launch_bounds__(WAVES * 64) void attn_rows_kernel(
                     const u32x4 w = reinterpret_cast<const u32x4*>(kb)[i * 4 + g];
 #pragma unroll
                     for (int kk = 0; kk < 4; ++kk) x.k[p][kk] = w[kk];
-                    x.ks[p] = kb[CODES + i * 4 + g];
                 } else {
                     const u32x2 w = reinterpret_cast<const u32x2*>(kb)[i * 4 + g];
                     x.k[p][0] = w.x;
                     x.k[p][1] = w.y;
-                    x.ks[p] = kb[CODES + i * 2 + (g >> 1)];
                 }
+                x.ks[p] = reinterpret_cast<const unsigned*>(kb + CODES)[HD == 128 ? i : i >> 1];
                 x.v[p] = reinterpret_cast<const u32x4*>(vb)[v_chunk * 4 + g];
                 x.vs[p] = reinterpret_cast<const unsigned*>(vb + CODES)[v_group * 4 + g];
             }
         };
         auto compute = [&](int n, Piece<HD>& x) {
             const int key0 = (s_begin + n * WAVES) * STEP;
-            f32x4 s[2];
+            f32x4 s[NR][2];
 #pragma unroll
             for (int p = 0; p < 2; ++p) {
-                const float ks = kv4_scale<0>(x.ks[p]);
-                s[p] = f32x4{0.f, 0.f, 0.f, 0.f};
+                const float ks = __uint_as_float(__builtin_amdgcn_alignbit(x.ks[p], x.ks[p], k_turn));   // the byte to bits 23 to 30
 #pragma unroll
-                for (int kk = 0; kk < KS; ++kk)
-                    s[p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kv4_eight(x.k[p][kk], ks)), qf[kk], s[p], 0, 0, 0);
+                for (int a = 0; a < NR; ++a) s[a][p] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int kk = 0; kk < KS; ++kk) {
+                    const bf16x8 kf = __builtin_bit_cast(bf16x8, kv4_eight(x.k[p][kk], ks));
+#pragma unroll
+                    for (int a = 0; a < NR; ++a) s[a][p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[a][kk], s[a][p], 0, 0, 0);
+                }
             }
             if (key0 + STEP - 1 > vis_min) {   // some row does not see all of these keys
 #pragma unroll
@@ -153,7 +176,9 @@ __global__ __launch_bounds__(WAVES * 64) void attn_rows_kernel(
                     const int k4 = key0 + p * LAPS_PAGE + 4 * g;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        if (k4 + e > limit) s[p][e] = -INFINITY;   // whatever it was, NaN included
+#pragma unroll
+                        for (int a = 0; a < NR; ++a)
+                            if (k4 + e > limit[a]) s[a][p][e] = -INFINITY;   // whatever it was, NaN included
                         // V of a key that a row does not see has weight zero, which a NaN would survive: slots past the sequence's end
                         // hold anything, and a NaN group of a key before it shows in the rows that see it only
                         const unsigned byte = (x.vs[p] >> (8 * e)) & 255u;
@@ -165,30 +190,43 @@ __global__ __launch_bounds__(WAVES * 64) void attn_rows_kernel(
                     }
                 }
             }
-            float mx = fmaxf(fmaxf(fmaxf(s[0].x, s[0].y), fmaxf(s[0].z, s[0].w)), fmaxf(fmaxf(s[1].x, s[1].y), fmaxf(s[1].z, s[1].w))) * scale_log2e;
             // The reference that the exponentials subtract follows the row's maximum only when that has grown by more than
             // RESCALE_SLACK (weights stay below 2^RESCALE_SLACK; the quotient does not depend on it): the exchange between a row's four
             // lanes and the rescale of O are rare.
-            if (__builtin_amdgcn_ballot_w64(mx > m_run + RESCALE_SLACK) != 0) {
-                mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-                mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-                const float m_new = fmaxf(m_run, mx);
-                const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
-                l_run *= alpha;
+            float mx[NR];
+            bool grown = false;
 #pragma unroll
-                for (int j = 0; j < DL; ++j) o[j] *= alpha;
-                m_run = m_new;
+            for (int a = 0; a < NR; ++a) {
+                mx[a] = fmaxf(fmaxf(fmaxf(s[a][0].x, s[a][0].y), fmaxf(s[a][0].z, s[a][0].w)),
+                              fmaxf(fmaxf(s[a][1].x, s[a][1].y), fmaxf(s[a][1].z, s[a][1].w))) * scale_log2e;
+                grown = grown || mx[a] > m_run[a] + RESCALE_SLACK;
             }
-            const float m_sub = m_run == -INFINITY ? 0.f : m_run;   // a row that has seen no key yet
-            bf16x8 pf;
+            if (__builtin_amdgcn_ballot_w64(grown) != 0) {
 #pragma unroll
-            for (int p = 0; p < 2; ++p)
+                for (int a = 0; a < NR; ++a) {
+                    mx[a] = fmaxf(mx[a], __shfl_xor(mx[a], 16, 64));
+                    mx[a] = fmaxf(mx[a], __shfl_xor(mx[a], 32, 64));
+                    const float m_new = fmaxf(m_run[a], mx[a]);
+                    const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[a] - m_new);
+                    l_run[a] *= alpha;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[p][e], scale_log2e, -m_sub));
-                    l_run += w;
-                    pf[4 * p + e] = (__bf16)w;
+                    for (int j = 0; j < DL; ++j) o[a][j] *= alpha;
+                    m_run[a] = m_new;
                 }
+            }
+            bf16x8 pf[NR];
+#pragma unroll
+            for (int a = 0; a < NR; ++a) {
+                const float m_sub = m_run[a] == -INFINITY ? 0.f : m_run[a];   // a row that has seen no key yet
+#pragma unroll
+                for (int p = 0; p < 2; ++p)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[a][p][e], scale_log2e, -m_sub));
+                        l_run[a] += w;
+                        pf[a][4 * p + e] = (__bf16)w;
+                    }
+            }
             // codes of one head_dim pair of the eight keys, then the keys side by side
             auto pair_of_keys = [&](auto B) {
                 constexpr int b = decltype(B)::value;
@@ -207,8 +245,11 @@ __global__ __launch_bounds__(WAVES * 64) void attn_rows_kernel(
                     lo[k] = __builtin_amdgcn_perm(w[2 * k + 1], w[2 * k], 0x05040100u);
                     hi[k] = __builtin_amdgcn_perm(w[2 * k + 1], w[2 * k], 0x07060302u);
                 }
-                o[2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), pf, o[2 * b], 0, 0, 0);
-                o[2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), pf, o[2 * b + 1], 0, 0, 0);
+#pragma unroll
+                for (int a = 0; a < NR; ++a) {
+                    o[a][2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), pf[a], o[a][2 * b], 0, 0, 0);
+                    o[a][2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), pf[a], o[a][2 * b + 1], 0, 0, 0);
+                }
             };
             pair_of_keys(std::integral_constant<int, 0>{});
             pair_of_keys(std::integral_constant<int, 1>{});
@@ -217,73 +258,89 @@ __global__ __launch_bounds__(WAVES * 64) void attn_rows_kernel(
                 pair_of_keys(std::integral_constant<int, 3>{});
             }
         };
-        // the next step is on its way while this one is worked on; two buffers in turn
-        Piece<HD> a, b;
-        if (n_steps > 0) load(0, a);
-        for (int n = 0; n < n_steps; n += 2) {
-            if (n + 1 < n_steps) load(n + 1, b);
-            compute(n, a);
-            if (n + 1 >= n_steps) break;
-            if (n + 2 < n_steps) load(n + 2, a);
-            compute(n + 1, b);
+        // The next step is on its way while one is worked on; two buffers in turn.  Past the last step the last one is loaded again:
+        // with a branch round the loads every wait would be for all of them.
+        if (n_steps > 0) {
+            Piece<HD> x, y;
+            auto load_at = [&](int n, Piece<HD>& to) { load(n < n_steps ? n : n_steps - 1, to); };
+            load_at(0, x);
+#pragma unroll
+            for (int a = 0; a < NR; ++a)
+#pragma unroll
+                for (int kk = 0; kk < KS; ++kk) asm volatile("" : "+v"(qf[a][kk]));   // as ids: the loop must find Q arrived
+            for (int n = 0;;) {
+                load_at(n + 1, y);
+                __builtin_amdgcn_sched_barrier(0);   // loads first: mixed with the work, their registers get copied behind waits
+                compute(n, x);
+                if (++n >= n_steps) break;
+                load_at(n + 1, x);
+                __builtin_amdgcn_sched_barrier(0);
+                compute(n, y);
+                if (++n >= n_steps) break;
+            }
         }
 
         // ---- NaN groups of keys that not every row sees
         nan_key = min(nan_key, __shfl_xor(nan_key, 16, 64));
         nan_key = min(nan_key, __shfl_xor(nan_key, 32, 64));
-        if (__shfl(nan_key, o_group * (KV4_GROUP / DL), 64) <= limit) {
+        const int nan_from = __shfl(nan_key, o_group * (KV4_GROUP / DL), 64);
 #pragma unroll
-            for (int j = 0; j < DL; ++j) o[j] += __builtin_nanf("");
-        }
-        // ---- the four waves' results: lane (i, g) holds row i, head_dim indices 4 DL g + DL e + j
-        l_run += __shfl_xor(l_run, 16, 64);
-        l_run += __shfl_xor(l_run, 32, 64);
-        __syncthreads();   // the row block before is read
+        for (int a = 0; a < NR; ++a) {
+            if (rb * ROWS + 16 * a >= n_rows) break;
+            if (nan_from <= limit[a]) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-#pragma unroll
-            for (int j = 0; j < DL; j += 4)
-                *reinterpret_cast<f32x4*>(&red_o[wave][i][(4 * g + e) * DL + j]) = f32x4{o[j][e], o[j + 1][e], o[j + 2][e], o[j + 3][e]};
-        if (g == 0) {
-            red_ml[wave][0][i] = m_run;
-            red_ml[wave][1][i] = l_run;
-        }
-        __syncthreads();
-        constexpr int PER = 16 * HD / (WAVES * 64);   // values a thread finishes
-        const int fr = tid / (HD / PER), fd = tid % (HD / PER) * PER, frow = rb * 16 + fr;
-        if (frow < n_rows) {
-            float m_all = red_ml[0][0][fr];
-#pragma unroll
-            for (int w = 1; w < WAVES; ++w) m_all = fmaxf(m_all, red_ml[w][0][fr]);
-            const float m_sub = m_all == -INFINITY ? 0.f : m_all;   // no key seen here, or NaN scores only
-            float l_all = 0.f, v[PER];
-#pragma unroll
-            for (int k = 0; k < PER; ++k) v[k] = 0.f;
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) {
-                const float f = __builtin_amdgcn_exp2f(red_ml[w][0][fr] - m_sub);
-                l_all += f * red_ml[w][1][fr];
-#pragma unroll
-                for (int k = 0; k < PER; ++k) v[k] += f * red_o[w][fr][fd + k];
+                for (int j = 0; j < DL; ++j) o[a][j] += __builtin_nanf("");
             }
-            const int ft = frow / G;
-            const size_t at = (size_t)(r.rs + ft) * n_q + kvh * G + frow - ft * G;   // (row, query head) of the batch
-            if (used == 1) {
-                const float inv = 1.f / l_all;
+            // ---- the four waves' results: lane (i, g) holds row i, head_dim indices 4 DL g + DL e + j
+            l_run[a] += __shfl_xor(l_run[a], 16, 64);
+            l_run[a] += __shfl_xor(l_run[a], 32, 64);
+            __syncthreads();   // the rows before are read
 #pragma unroll
-                for (int k = 0; k < PER; k += 4) {
-                    u32x2 w;
-                    w.x = pack_bf16x2(v[k] * inv, v[k + 1] * inv);
-                    w.y = pack_bf16x2(v[k + 2] * inv, v[k + 3] * inv);
-                    *reinterpret_cast<u32x2*>(out + at * HD + fd + k) = w;
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int j = 0; j < DL; j += 4)
+                    *reinterpret_cast<f32x4*>(&red_o[wave][i][(4 * g + e) * DL + j]) = f32x4{o[a][j][e], o[a][j + 1][e], o[a][j + 2][e], o[a][j + 3][e]};
+            if (g == 0) {
+                red_ml[wave][0][i] = m_run[a];
+                red_ml[wave][1][i] = l_run[a];
+            }
+            __syncthreads();
+            constexpr int PER = 16 * HD / (WAVES * 64);   // values a thread finishes
+            const int fr = tid / (HD / PER), fd = tid % (HD / PER) * PER, frow = rb * ROWS + 16 * a + fr;
+            if (frow < n_rows) {
+                float m_all = red_ml[0][0][fr];
+#pragma unroll
+                for (int w = 1; w < WAVES; ++w) m_all = fmaxf(m_all, red_ml[w][0][fr]);
+                const float m_sub = m_all == -INFINITY ? 0.f : m_all;   // no key seen here, or NaN scores only
+                float l_all = 0.f, v[PER];
+#pragma unroll
+                for (int k = 0; k < PER; ++k) v[k] = 0.f;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) {
+                    const float f = __builtin_amdgcn_exp2f(red_ml[w][0][fr] - m_sub);
+                    l_all += f * red_ml[w][1][fr];
+#pragma unroll
+                    for (int k = 0; k < PER; ++k) v[k] += f * red_o[w][fr][fd + k];
                 }
-            } else {
+                const int ft = frow / G;
+                const size_t at = (size_t)(r.rs + ft) * n_q + kvh * G + frow - ft * G;   // (row, query head) of the batch
+                if (used == 1) {
+                    const float inv = 1.f / l_all;
 #pragma unroll
-                for (int k = 0; k < PER; k += 4)
-                    *reinterpret_cast<f32x4*>(part_o + (at * parts + part) * HD + fd + k) = f32x4{v[k], v[k + 1], v[k + 2], v[k + 3]};
-                if (fd == 0) {
-                    part_ml[(at * parts + part) * 2] = m_all;
-                    part_ml[(at * parts + part) * 2 + 1] = l_all;
+                    for (int k = 0; k < PER; k += 4) {
+                        u32x2 w;
+                        w.x = pack_bf16x2(v[k] * inv, v[k + 1] * inv);
+                        w.y = pack_bf16x2(v[k + 2] * inv, v[k + 3] * inv);
+                        *reinterpret_cast<u32x2*>(out + at * HD + fd + k) = w;
+                    }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < PER; k += 4)
+                        *reinterpret_cast<f32x4*>(part_o + (at * parts + part) * HD + fd + k) = f32x4{v[k], v[k + 1], v[k + 2], v[k + 3]};
+                    if (fd == 0) {
+                        part_ml[(at * parts + part) * 2] = m_all;
+                        part_ml[(at * parts + part) * 2 + 1] = l_all;
+                    }
                 }
             }
         }
@@ -297,18 +354,23 @@ __global__ __launch_bounds__(8 * HD / 4) void attn_rows_merge_kernel(bf16_t* __r
                                                                      const float* __restrict__ part_ml, const int* __restrict__ cu,
                                                                      const int* __restrict__ seq_len,
                                                                      const int* __restrict__ prefix_len, int max_pages,
-                                                                     int n_tokens, int n_q, int parts) {
+                                                                     int n_tokens, int n_q, int parts, int min_parts) {
     constexpr int LANES = HD / 4, GROUPS = 8;
-    __shared__ float weight[MAX_PARTS], sum[MAX_PARTS];
+    __shared__ float weight[MAX_PARTS], l_all;
     __shared__ f32x4 red[GROUPS][LANES];
     const int head = blockIdx.x % n_q, seq = blockIdx.x / n_q, tid = threadIdx.x, c = tid % LANES, grp = tid / LANES;
     SeqRange r;
     if (!seq_range(seq, cu, seq_len, prefix_len, n_tokens, max_pages, &r)) return;
     int used;
-    part_steps(r.H + r.L, parts, &used);
+    part_steps(r.H + r.L, max_pages, parts, min_parts, &used);
     if (used == 1) return;   // written by the attention kernel
     for (int t = blockIdx.y; t < r.L; t += gridDim.y) {
         const size_t at = ((size_t)(r.rs + t) * n_q + head) * parts;
+        const int run = (used + GROUPS - 1) / GROUPS, p0 = grp * run;   // at most 8 parts a group, all on their way before any is used
+        f32x4 v[MAX_PARTS / GROUPS];
+#pragma unroll
+        for (int p = 0; p < MAX_PARTS / GROUPS; ++p)
+            if (p < run) v[p] = reinterpret_cast<const f32x4*>(part_o + (at + (p0 + p < used ? p0 + p : used - 1)) * HD)[c];
         if (tid < 64) {   // parts <= 64: one a lane
             const float m = tid < used ? part_ml[(at + tid) * 2] : -INFINITY, l = tid < used ? part_ml[(at + tid) * 2 + 1] : 0.f;
             float m_all = m;
@@ -316,21 +378,22 @@ __global__ __launch_bounds__(8 * HD / 4) void attn_rows_merge_kernel(bf16_t* __r
             for (int k = 32; k > 0; k >>= 1) m_all = fmaxf(m_all, __shfl_xor(m_all, k, 64));
             const float f = __builtin_amdgcn_exp2f(m - (m_all == -INFINITY ? 0.f : m_all));
             weight[tid] = f;
-            sum[tid] = f * l;
+            float sum = f * l;
+#pragma unroll
+            for (int k = 32; k > 0; k >>= 1) sum += __shfl_xor(sum, k, 64);
+            if (tid == 0) l_all = sum;
         }
         __syncthreads();
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-        const int run = (used + GROUPS - 1) / GROUPS, p1 = (grp + 1) * run < used ? (grp + 1) * run : used;
-#pragma unroll 8
-        for (int p = grp * run; p < p1; ++p) acc += weight[p] * reinterpret_cast<const f32x4*>(part_o + (at + p) * HD)[c];
+#pragma unroll
+        for (int p = 0; p < MAX_PARTS / GROUPS; ++p)
+            if (p < run && p0 + p < used) acc += weight[p0 + p] * v[p];
         red[grp][c] = acc;
         __syncthreads();
         if (grp == 0) {
-            float l = 0.f;
-            for (int p = 0; p < used; ++p) l += sum[p];
 #pragma unroll
             for (int k = 1; k < GROUPS; ++k) acc += red[k][c];
-            const float inv = 1.f / l;
+            const float inv = 1.f / l_all;
             u32x2 w;
             w.x = pack_bf16x2(acc.x * inv, acc.y * inv);
             w.y = pack_bf16x2(acc.z * inv, acc.w * inv);
@@ -340,18 +403,75 @@ __global__ __launch_bounds__(8 * HD / 4) void attn_rows_merge_kernel(bf16_t* __r
     }
 }
 
+// The same for at most FEW_PARTS parts: HD / 4 lanes take a (row, query head), all its parts at once, no exchange between lanes.
+constexpr int FEW_PARTS = 8, FEW_THREADS = 256;
+template <int HD>
+__global__ __launch_bounds__(FEW_THREADS) void attn_rows_merge_few_kernel(bf16_t* __restrict__ out, const float* __restrict__ part_o,
+                                                                          const float* __restrict__ part_ml,
+                                                                          const int* __restrict__ cu, const int* __restrict__ seq_len,
+                                                                          const int* __restrict__ prefix_len, int max_pages,
+                                                                          int n_tokens, int n_q, int parts, int min_parts) {
+    constexpr int LANES = HD / 4, GROUPS = FEW_THREADS / LANES;
+    const int seq = blockIdx.x, c = threadIdx.x % LANES;
+    SeqRange r;
+    if (!seq_range(seq, cu, seq_len, prefix_len, n_tokens, max_pages, &r)) return;
+    int used;
+    part_steps(r.H + r.L, max_pages, parts, min_parts, &used);
+    if (used == 1) return;   // written by the attention kernel
+    const long items = (long)r.L * n_q, first = (long)r.rs * n_q;
+    for (long it = (long)blockIdx.y * GROUPS + threadIdx.x / LANES; it < items; it += (long)gridDim.y * GROUPS) {
+        const size_t at = (size_t)(first + it) * parts;
+        f32x4 v[FEW_PARTS];
+        float m[FEW_PARTS], l[FEW_PARTS];
+#pragma unroll
+        for (int p = 0; p < FEW_PARTS; ++p) {
+            m[p] = -INFINITY;
+            l[p] = 0.f;
+            v[p] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (p < used) {
+                v[p] = reinterpret_cast<const f32x4*>(part_o + (at + p) * HD)[c];
+                m[p] = part_ml[(at + p) * 2];
+                l[p] = part_ml[(at + p) * 2 + 1];
+            }
+        }
+        float m_all = m[0];
+#pragma unroll
+        for (int p = 1; p < FEW_PARTS; ++p) m_all = fmaxf(m_all, m[p]);
+        const float m_sub = m_all == -INFINITY ? 0.f : m_all;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        float l_all = 0.f;
+#pragma unroll
+        for (int p = 0; p < FEW_PARTS; ++p) {
+            const float f = __builtin_amdgcn_exp2f(m[p] - m_sub);
+            acc += f * v[p];
+            l_all += f * l[p];
+        }
+        const float inv = 1.f / l_all;
+        u32x2 w;
+        w.x = pack_bf16x2(acc.x * inv, acc.y * inv);
+        w.y = pack_bf16x2(acc.z * inv, acc.w * inv);
+        *reinterpret_cast<u32x2*>(out + (first + it) * HD + 4 * c) = w;
+    }
+}
+
 template <int HD>
 int launch_rows(const Kv4Attn& a, const Kv4RowsPlan& p, float* part, hipStream_t s) {
     const float scale_log2e = 1.4426950408889634f / sqrtf((float)HD);
     float* part_ml = part ? part + (size_t)a.n_tokens * a.n_q * p.parts * HD : nullptr;
-    hipLaunchKernelGGL(attn_rows_kernel<HD>, dim3(a.n_kv * p.row_blocks * a.n_seq, p.parts), dim3(WAVES * 64), 0, s, a.q, a.out, a.k_pool,
-                       a.v_pool, a.cu, a.seq_len, a.prefix_len, a.page_table, a.max_pages, a.n_tokens, a.n_q, a.n_kv, a.n_pool_pages,
-                       p.row_blocks, p.parts, scale_log2e, part, part_ml);
+    auto kern = p.row_tiles == 1 ? attn_rows_kernel<HD, 1> : attn_rows_kernel<HD, 2>;
+    hipLaunchKernelGGL(kern, dim3((a.n_seq * p.parts * p.row_blocks + 7) / 8 * 8 * a.n_kv), dim3(WAVES * 64), 0, s, a.q, a.out, a.k_pool,
+                       a.v_pool, a.cu, a.seq_len, a.prefix_len, a.page_table, a.max_pages, a.n_seq, a.n_tokens, a.n_q, a.n_kv, a.n_pool_pages,
+                       p.row_blocks, p.parts, p.min_parts, scale_log2e, part, part_ml);
     LAPS_LAUNCH_CHECK();
-    if (p.parts > 1) {
-        const int rows = (a.n_tokens + a.n_seq - 1) / a.n_seq;
+    const int rows = (a.n_tokens + a.n_seq - 1) / a.n_seq;   // of a sequence, in the mean
+    if (p.parts > FEW_PARTS) {
         hipLaunchKernelGGL(attn_rows_merge_kernel<HD>, dim3(a.n_q * a.n_seq, rows < 64 ? rows : 64), dim3(8 * HD / 4), 0, s, a.out, part, part_ml,
-                           a.cu, a.seq_len, a.prefix_len, a.max_pages, a.n_tokens, a.n_q, p.parts);
+                           a.cu, a.seq_len, a.prefix_len, a.max_pages, a.n_tokens, a.n_q, p.parts, p.min_parts);
+        LAPS_LAUNCH_CHECK();
+    } else if (p.parts > 1) {
+        const long wgs = ((long)rows * a.n_q * HD / 4 + FEW_THREADS - 1) / FEW_THREADS;
+        hipLaunchKernelGGL(attn_rows_merge_few_kernel<HD>, dim3(a.n_seq, wgs < 4096 ? wgs : 4096), dim3(FEW_THREADS), 0, s, a.out, part, part_ml,
+                           a.cu, a.seq_len, a.prefix_len, a.max_pages, a.n_tokens, a.n_q, p.parts, p.min_parts);
         LAPS_LAUNCH_CHECK();
     }
     return LAPS_OK;
@@ -359,23 +479,31 @@ int launch_rows(const Kv4Attn& a, const Kv4RowsPlan& p, float* part, hipStream_t
 
 }  // namespace
 
-// Blocks of 128 rows read and unpack the keys once for all of them, but pay for 128 whatever they hold, and for their work-item
-// table.  This kernel against blocks, graph replays, us: 32B, 16 sequences over 2048 keys, 4 / 6 / 8 / 16 tokens each 29 / 32 / 43 / 63
-// and 36 / 37 / 42 / 42; one over 4000 keys, 1 / 8 / 16 tokens 9.6 / 16.4 / 22.7 and 16.8 / 17.6 / 18.5.
+// Blocks of 128 or 256 rows read and unpack the keys once for all of them, but pay for their padding, their longer fill and their
+// work-item table; here every 32 rows unpack them again.  This kernel / blocks, graph replays, us: 32B, 16 sequences of 4 / 16 / 64 / 96
+// tokens over 2048 keys 18 / 31 / 73 / 109 and 37 / 44 / 80 / 90 (128 to 1920 workgroups), 64 of 8 / 16 / 24 over 2000 58 / 84 / 111 and
+// 80 / 88 / 94 (1024 to 2048), of 8 / 16 over 300 22 / 30 and 21 / 24; one of 128 over 16000 70 and 100 (160).
 bool laps_kv4_takes_rows(int n_seq, int n_tokens, int n_q, int n_kv) {
-    return (long)n_tokens * (n_q / n_kv) <= 32L * n_seq;
+    const long rows = (long)n_tokens * (n_q / n_kv), blocks = (rows + 32L * n_seq - 1) / (32L * n_seq);
+    return rows <= 16L * n_seq || blocks * n_seq * n_kv <= 1024;
 }
 
 Kv4RowsPlan laps_kv4_rows_plan(int n_seq, int n_tokens, int n_q, int n_kv, int max_pages) {
     const long rows = (long)n_tokens * (n_q / n_kv);
-    long blocks = (rows + 16L * n_seq - 1) / (16L * n_seq);
+    const int tiles = rows > 16L * n_seq ? 2 : 1;
+    long blocks = (rows + 16L * tiles * n_seq - 1) / (16L * tiles * n_seq);
     const long most = (1L << 20) / ((long)n_seq * n_kv);   // a grid of a million workgroups at most; they walk the blocks that are left
     blocks = blocks < most ? blocks : (most > 1 ? most : 1);
     const long rounds = ((long)max_pages * LAPS_PAGE + STEP * WAVES - 1) / (STEP * WAVES);   // of the longest sequence the table holds
-    long parts = (2048 + blocks * n_seq * n_kv - 1) / (blocks * n_seq * n_kv);
-    parts = parts < rounds ? parts : rounds;
-    parts = parts < MAX_PARTS ? parts : MAX_PARTS;
-    return {(int)blocks, (int)(parts < 1 ? 1 : parts)};
+    // One resident workgroup a place on the chip (3 or 2 a unit) where the sequences are alike; twice as many parts at most where
+    // the table allows sequences long enough for the longest one to outlast the others and a part to be worth the merge.  32B,
+    // 64 tokens over 4096 keys each, 1 / 2 / 4 parts 47.8 / 51.3 / 58 us; over 512 to 8191 70.1 / 68.3 / 72, up to 3 by length 64.7;
+    // 96 over 16 to 1300 1 / 2 parts 20.5 / 26.2.
+    const long units = blocks * n_seq * n_kv, places = tiles == 1 ? 768 : 256;
+    auto within = [&](long n, long most) { return n < most ? n : most; };
+    const long min_parts = within(within(places / units, rounds), MAX_PARTS);
+    const long parts = within(within(2 * places / units, rounds / (tiles == 1 ? 16 : 8)), MAX_PARTS);
+    return {tiles, (int)blocks, (int)(parts > min_parts ? parts : (min_parts > 1 ? min_parts : 1)), (int)(min_parts > 1 ? min_parts : 1)};
 }
 
 size_t laps_kv4_rows_bytes(const Kv4RowsPlan& p, int n_tokens, int n_q, int hd) {

@@ -70,8 +70,10 @@ struct Kv4Attn {
 };
 // Launch of the kernel for few query rows a sequence.
 struct Kv4RowsPlan {
+    int row_tiles;    // 16-row tiles of a block
     int row_blocks;   // blocks of rows that workgroups of their own walk, a sequence and kv head
     int parts;        // most parts of a sequence's keys
+    int min_parts;    // as many at least, where there are keys for them
 };
 // Which of the two kernels a launch shape takes: this one, or the blocks of 128 or 256 rows of the bf16 pools' attention.
 bool laps_kv4_takes_rows(int n_seq, int n_tokens, int n_q, int n_kv);
