@@ -128,15 +128,16 @@ def _after_current(stream):
 
 def _held_by(stream, *tensors):
     """Tensors made on the current stream for work on `stream`: their memory goes to nobody else before that is done."""
-    if stream is not None and stream.cuda_stream != torch.cuda.current_stream().cuda_stream:
+    if stream.cuda_stream != torch.cuda.current_stream().cuda_stream:
         for t in tensors:
             t.record_stream(stream)
 
 
-def _expect(what, t, dtype, *shape):
+def _expect(what, t, dtype, shape, device):
     """Refuses a tensor that a kernel would read past or misread; returns its address."""
-    if t.dtype is not dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
-        raise LapsError(f"{what}: need a contiguous {dtype} device tensor of shape {list(shape)}, got {t.dtype} {list(t.shape)} on {t.device}")
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or device < 0 or not t.is_contiguous():
+        raise LapsError(f"{what}: need a contiguous {dtype} tensor of shape {list(shape)} on the GPU of k4_pool, "
+                        f"got {t.dtype} {list(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
@@ -470,49 +471,45 @@ class LapsCtx:
         k4, v4 = ([mk(shape, dtype=torch.uint8, device="cuda") for _ in range(n_layers or self.cfg.n_layers)] for _ in range(2))
         return k4, v4
 
-    def _kv4_call(self, cu, per_seq, page_table, k4_pool, v4_pool):
-        """Checks what every call on 4-bit pools takes; returns the sequences, the table's width, the arrays' addresses and
-        their device."""
-        n_seq, width = cu.numel() - 1, page_table.shape[-1]
-        at = [_expect("cu", cu, torch.int32, n_seq + 1)]
-        at += [0 if t is None else _expect(what, t, torch.int32, n_seq) for what, t in per_seq]
-        at.append(_expect("page_table", page_table, torch.int32, n_seq, width))
-        at += [_expect(what, t, torch.uint8, k4_pool.shape[0], self.cfg.n_kv_heads, self._kv4_block)
-               for what, t in (("k4_pool", k4_pool), ("v4_pool", v4_pool))]
-        return n_seq, width, at, k4_pool.get_device()
-
-    @staticmethod
-    def _same_device(device, *tensors):
-        if any(t is not None and t.get_device() != device for t in tensors):
-            raise LapsError("tensors of one call on different devices")
+    def _kv4_call(self, cu, page_table, k4_pool, v4_pool):
+        """Checks what every call on 4-bit pools takes: returns the sequences, the table's width, the pools' device and the
+        arrays' addresses."""
+        n_seq, width, device = cu.numel() - 1, page_table.shape[-1], k4_pool.get_device()
+        pools = (k4_pool.shape[0], self.cfg.n_kv_heads, self._kv4_block)
+        return (n_seq, width, device, _expect("cu", cu, torch.int32, (n_seq + 1,), device),
+                _expect("page_table", page_table, torch.int32, (n_seq, width), device),
+                _expect("k4_pool", k4_pool, torch.uint8, pools, device), _expect("v4_pool", v4_pool, torch.uint8, pools, device))
 
     def _kv4_stream(self, stream, k4_pool, device):
         self._guard_pools(k4_pool)
+        if stream is None:
+            return torch.cuda.current_stream(device).cuda_stream
         _after_current(stream)
-        return (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
+        return stream.cuda_stream
 
     def laps_kv4_scatter(self, cu, start_pos, page_table, k_src, v_src, k4_pool, v4_pool, stream=None):
         """Quantises token-major bf16 K/V [n_tokens, n_kv_heads, head_dim] into 4-bit pools (new_kv4_pools)."""
-        n_seq, width, (cu_p, start_p, table_p, k_p, v_p), device = self._kv4_call(cu, (("start_pos", start_pos),), page_table, k4_pool, v4_pool)
+        n_seq, width, device, cu_p, table_p, k_p, v_p = self._kv4_call(cu, page_table, k4_pool, v4_pool)
         shape = (k_src.shape[0], self.cfg.n_kv_heads, self.cfg.head_dim)
-        src = _expect("k_src", k_src, torch.bfloat16, *shape), _expect("v_src", v_src, torch.bfloat16, *shape)
-        self._same_device(device, cu, start_pos, page_table, v4_pool, k_src, v_src)
+        start_p = _expect("start_pos", start_pos, torch.int32, (n_seq,), device)
+        src_k, src_v = _expect("k_src", k_src, torch.bfloat16, shape, device), _expect("v_src", v_src, torch.bfloat16, shape, device)
         s = self._kv4_stream(stream, k4_pool, device)
-        _check(lib().laps_kv4_scatter(self._h, n_seq, shape[0], cu_p, start_p, table_p, width, *src, k_p, v_p, s))
+        _check(lib().laps_kv4_scatter(self._h, n_seq, shape[0], cu_p, start_p, table_p, width, src_k, src_v, k_p, v_p, s))
 
     def laps_kv4_gather(self, cu, start_pos, page_table, k4_pool, v4_pool, n_tokens, k_out=None, v_out=None, stream=None):
         """Reads token-major bf16 K/V back from 4-bit pools, into k_out / v_out if given.  Rows without a page keep what they
         held (nothing defined in tensors made here)."""
-        n_seq, width, (cu_p, start_p, table_p, k_p, v_p), device = self._kv4_call(cu, (("start_pos", start_pos),), page_table, k4_pool, v4_pool)
+        n_seq, width, device, cu_p, table_p, k_p, v_p = self._kv4_call(cu, page_table, k4_pool, v4_pool)
         shape = (n_tokens, self.cfg.n_kv_heads, self.cfg.head_dim)
-        made = [t is None for t in (k_out, v_out)]
-        outs = [torch.empty(shape, dtype=torch.bfloat16, device=k4_pool.device) if t is None else t for t in (k_out, v_out)]
-        dst = [_expect(what, t, torch.bfloat16, *shape) for what, t in zip(("k_out", "v_out"), outs)]
-        self._same_device(device, cu, start_pos, page_table, v4_pool, *outs)
+        start_p = _expect("start_pos", start_pos, torch.int32, (n_seq,), device)
+        k = torch.empty(shape, dtype=torch.bfloat16, device=k4_pool.device) if k_out is None else k_out
+        v = torch.empty(shape, dtype=torch.bfloat16, device=k4_pool.device) if v_out is None else v_out
+        dst_k, dst_v = _expect("k_out", k, torch.bfloat16, shape, device), _expect("v_out", v, torch.bfloat16, shape, device)
         s = self._kv4_stream(stream, k4_pool, device)
-        _check(lib().laps_kv4_gather(self._h, n_seq, n_tokens, cu_p, start_p, table_p, width, k_p, v_p, *dst, s))
-        _held_by(stream, *(t for t, m in zip(outs, made) if m))
-        return outs[0], outs[1]
+        _check(lib().laps_kv4_gather(self._h, n_seq, n_tokens, cu_p, start_p, table_p, width, k_p, v_p, dst_k, dst_v, s))
+        if stream is not None:
+            _held_by(stream, *(t for t, given in ((k, k_out), (v, v_out)) if given is None))
+        return k, v
 
     def laps_attention_kv4_workspace_bytes(self, n_seq: int, n_tokens: int, max_pages: int) -> int:
         return lib().laps_attention_kv4_workspace_bytes(self._h, n_seq, n_tokens, max_pages)
@@ -520,21 +517,21 @@ class LapsCtx:
     def laps_attention_kv4(self, cu, seq_len, prefix_len, page_table, k4_pool, v4_pool, q, out=None, stream=None):
         """laps_attention over 4-bit pools.  Rows of `out` that hold no token keep what they held (zeros if made here).  The
         workspace is this call's own: calls on several streams and captured graphs do not share one."""
-        n_seq, width, (cu_p, len_p, pre_p, table_p, k_p, v_p), device = self._kv4_call(
-            cu, (("seq_len", seq_len), ("prefix_len", prefix_len)), page_table, k4_pool, v4_pool)
+        n_seq, width, device, cu_p, table_p, k_p, v_p = self._kv4_call(cu, page_table, k4_pool, v4_pool)
         shape = (q.shape[0], self.cfg.n_q_heads * self.cfg.head_dim)
-        q_p = _expect("q", q, torch.bfloat16, *shape)
-        made = out is None
-        out = torch.zeros_like(q) if made else out
-        out_p = _expect("out", out, torch.bfloat16, *shape)
-        self._same_device(device, cu, seq_len, prefix_len, page_table, v4_pool, q, out)
-        need = self.laps_attention_kv4_workspace_bytes(n_seq, shape[0], width)
-        ws = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+        len_p = None if seq_len is None else _expect("seq_len", seq_len, torch.int32, (n_seq,), device)
+        pre_p = _expect("prefix_len", prefix_len, torch.int32, (n_seq,), device)
+        q_p = _expect("q", q, torch.bfloat16, shape, device)
+        y = torch.zeros_like(q) if out is None else out
+        y_p = _expect("out", y, torch.bfloat16, shape, device)
+        need = lib().laps_attention_kv4_workspace_bytes(self._h, n_seq, shape[0], width)
+        ws = torch.empty(need or 256, dtype=torch.uint8, device=q.device)
         s = self._kv4_stream(stream, k4_pool, device)
-        _check(lib().laps_attention_kv4(self._h, n_seq, shape[0], cu_p, len_p, pre_p, table_p, width, k_p, v_p, q_p, out_p,
+        _check(lib().laps_attention_kv4(self._h, n_seq, shape[0], cu_p, len_p, pre_p, table_p, width, k_p, v_p, q_p, y_p,
                                         ws.data_ptr(), need, s))
-        _held_by(stream, ws, *((out,) if made else ()))
-        return out
+        if stream is not None:
+            _held_by(stream, ws, *((y,) if out is None else ()))
+        return y
 
     # ---- forward
     def laps_prefill_layer(self, w: dict, cu, seq_len, prefix_len, page_table, k_pool, v_pool, x_in, x_out=None,

@@ -78,8 +78,9 @@ def test_entry_points_refuse_a_missing_context():
 
 @pytest.mark.parametrize("t", [torch.zeros(4, 2), torch.zeros(4, 2, dtype=torch.int32), torch.zeros(2, 4, dtype=torch.int32).t()])
 def test_binding_refuses_other_tensors(t):
-    with pytest.raises(api.LapsError, match="page_table"):
-        api._expect("page_table", t, torch.int32, 4, 2)      # host memory, another type, not contiguous
+    for device in (-1, 0):
+        with pytest.raises(api.LapsError, match="page_table"):
+            api._expect("page_table", t, torch.int32, (4, 2), device)      # host memory, another type, not contiguous
 
 
 def test_model_shapes_have_whole_groups():
