@@ -27,7 +27,7 @@ namespace {
 constexpr int WAVES = 4;
 constexpr int STEP = 2 * LAPS_PAGE;   // keys a wave takes at a time
 constexpr int MAX_PARTS = 64;
-constexpr float RESCALE_SLACK = 8.f;  // log2; see below
+constexpr float MOST = 256.f;   // sum of eight weights above which the reference moves
 
 typedef unsigned char byte_t;
 
@@ -190,43 +190,51 @@ __global__ __launch_bounds__(WAVES * 64, NR == 1 ? 3 : 2) void attn_rows_kernel(
                     }
                 }
             }
-            // The reference that the exponentials subtract follows the row's maximum only when that has grown by more than
-            // RESCALE_SLACK (weights stay below 2^RESCALE_SLACK; the quotient does not depend on it): the exchange between a row's four
-            // lanes and the rescale of O are rare.
-            float mx[NR];
-            bool grown = false;
+            // The reference that the exponentials subtract is the row's maximum as of some earlier step.  It moves when the weights it
+            // gives add up to more than MOST (or when there is none yet): no maximum is taken in the other steps, and the exchange between a
+            // row's four lanes and the rescale of O are rare.  The quotient O / l does not depend on it; weights stay far from
+            // float32's range, and since the maximum never falls below the reference, so does l.
+            bf16x8 pf[NR];
+            float sum[NR];   // of the weights as the second product sees them
+            auto weights = [&](int a) {
+                const float m_sub = m_run[a] == -INFINITY ? 0.f : m_run[a];   // a row that has seen no key yet
+                sum[a] = 0.f;
+#pragma unroll
+                for (int p = 0; p < 2; ++p)
+#pragma unroll
+                    for (int e = 0; e < 4; e += 2) {
+                        bf16x2 w;
+                        w.x = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[a][p][e], scale_log2e, -m_sub));
+                        w.y = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[a][p][e + 1], scale_log2e, -m_sub));
+                        pf[a][4 * p + e] = w.x;
+                        pf[a][4 * p + e + 1] = w.y;
+                        sum[a] = __builtin_amdgcn_fdot2_f32_bf16(w, bf16x2{(__bf16)1.f, (__bf16)1.f}, sum[a], false);
+                    }
+            };
+            bool move = false;
 #pragma unroll
             for (int a = 0; a < NR; ++a) {
-                mx[a] = fmaxf(fmaxf(fmaxf(s[a][0].x, s[a][0].y), fmaxf(s[a][0].z, s[a][0].w)),
-                              fmaxf(fmaxf(s[a][1].x, s[a][1].y), fmaxf(s[a][1].z, s[a][1].w))) * scale_log2e;
-                grown = grown || mx[a] > m_run[a] + RESCALE_SLACK;
+                weights(a);
+                move = move || sum[a] > MOST || m_run[a] == -INFINITY;
             }
-            if (__builtin_amdgcn_ballot_w64(grown) != 0) {
+            if (__builtin_amdgcn_ballot_w64(move) != 0) {
 #pragma unroll
                 for (int a = 0; a < NR; ++a) {
-                    mx[a] = fmaxf(mx[a], __shfl_xor(mx[a], 16, 64));
-                    mx[a] = fmaxf(mx[a], __shfl_xor(mx[a], 32, 64));
-                    const float m_new = fmaxf(m_run[a], mx[a]);
+                    float mx = fmaxf(fmaxf(fmaxf(s[a][0].x, s[a][0].y), fmaxf(s[a][0].z, s[a][0].w)),
+                                     fmaxf(fmaxf(s[a][1].x, s[a][1].y), fmaxf(s[a][1].z, s[a][1].w))) * scale_log2e;
+                    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+                    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+                    const float m_new = fmaxf(m_run[a], mx);
                     const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[a] - m_new);
                     l_run[a] *= alpha;
 #pragma unroll
                     for (int j = 0; j < DL; ++j) o[a][j] *= alpha;
                     m_run[a] = m_new;
+                    weights(a);
                 }
             }
-            bf16x8 pf[NR];
 #pragma unroll
-            for (int a = 0; a < NR; ++a) {
-                const float m_sub = m_run[a] == -INFINITY ? 0.f : m_run[a];   // a row that has seen no key yet
-#pragma unroll
-                for (int p = 0; p < 2; ++p)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[a][p][e], scale_log2e, -m_sub));
-                        l_run[a] += w;
-                        pf[a][4 * p + e] = (__bf16)w;
-                    }
-            }
+            for (int a = 0; a < NR; ++a) l_run[a] += sum[a];
             // codes of one head_dim pair of the eight keys, then the keys side by side
             auto pair_of_keys = [&](auto B) {
                 constexpr int b = decltype(B)::value;

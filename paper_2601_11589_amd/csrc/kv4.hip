@@ -6,15 +6,22 @@
 // One workgroup per (page of a sequence, kv head), 2 * head_dim threads, each eight values of K and eight of V.  K lies
 // [token][head_dim] on both sides, so consecutive threads take consecutive chunks and a group is four neighbouring lanes.  V's
 // codes lie [head_dim / 8][16 tokens][8 values] (what a lane of the attention reads is four tokens of the same eight head_dim
-// indices): thread t takes token t % 16 of chunk t / 16, so the pool side is one dword a thread in order and the token side 64-byte
-// pieces; a group is four lanes 16 apart.  No LDS, no barrier.
+// indices).  What is written goes out in whole lines: on the way in thread t takes token t % 16 of chunk t / 16 (the pool side in
+// order, the token side in 64-byte pieces, a group four lanes 16 apart), on the way out V is assigned as K is and the pool's dwords
+// are picked up from all over their kilobyte.  No LDS, no barrier.
+//
+// Token-major rows that the L2 caches do not hold stream past them.  37 k tokens of 8 heads x 128 (193 MB), cold: written 39.3 us, rows
+// read past the caches 35.3 (5.5 TB/s; a large copy 5.1); read back with V as on the way in 43.7, as K 39.3, and rows written past the
+// caches 30.8 (6.3 TB/s).  A few hundred tokens: the time of a launch, all ways.
 #include "kv4.h"
+
+#include <type_traits>
 
 namespace {
 
 // Work items as in the mover of the bf16 pools: the first item of sequence s is cu[s] / 16 + 2 s (a run of n tokens touches at most
 // n / 16 + 2 pages), items that no page needs return at once.
-template <int HD, bool SCATTER>
+template <int HD, bool SCATTER, bool STREAM>
 __global__ __launch_bounds__(2 * HD) void kv4_move_kernel(const int* __restrict__ cu, const int* __restrict__ start_pos,
                                                           const int* __restrict__ page_table, u32x4* __restrict__ k_tok,
                                                           u32x4* __restrict__ v_tok, unsigned char* __restrict__ k_pool,
@@ -40,14 +47,19 @@ __global__ __launch_bounds__(2 * HD) void kv4_move_kernel(const int* __restrict_
     if (page < 0 || page >= n_pool_pages) return;                      // unset table entry, or not a page of the pool
     const size_t block = ((size_t)page * n_kv + head) * kv4_block(HD);
     unsigned char *kb = k_pool + block, *vb = v_pool + block;
-    const int k_off = tid / CPR, k_c = tid % CPR, v_off = tid % LAPS_PAGE, v_c = tid / LAPS_PAGE;
+    const int k_off = tid / CPR, k_c = tid % CPR, v_off = SCATTER ? tid % LAPS_PAGE : k_off, v_c = SCATTER ? tid / LAPS_PAGE : k_c;
     const bool k_mine = k_off >= off0 && k_off < off1, v_mine = v_off >= off0 && v_off < off1;
     const size_t k_at = ((size_t)(a + k_off) * n_kv + head) * CPR + k_c, v_at = ((size_t)(a + v_off) * n_kv + head) * CPR + v_c;
     unsigned char *k_scale = kb + CODES + k_off * GROUPS + k_c / 4, *v_scale = vb + CODES + (v_c / 4) * LAPS_PAGE + v_off;
+    auto take = [](const u32x4* from) { return STREAM ? __builtin_nontemporal_load(from) : *from; };
+    auto put = [](u32x4 x, u32x4* to) {
+        if (STREAM) __builtin_nontemporal_store(x, to);
+        else *to = x;
+    };
     if (SCATTER) {
         u32x4 k = {0u, 0u, 0u, 0u}, v = {0u, 0u, 0u, 0u};
-        if (k_mine) k = k_tok[k_at];
-        if (v_mine) v = v_tok[v_at];
+        if (k_mine) k = take(k_tok + k_at);
+        if (v_mine) v = take(v_tok + v_at);
         // the lanes of a group are all `mine` or none
         unsigned ka = kv4_amax(k), va = kv4_amax(v);
 #pragma unroll
@@ -66,10 +78,10 @@ __global__ __launch_bounds__(2 * HD) void kv4_move_kernel(const int* __restrict_
             if (v_c % 4 == 0) *v_scale = (unsigned char)vs;
         }
     } else {
-        const unsigned kc = reinterpret_cast<const unsigned*>(kb)[tid], vc = reinterpret_cast<const unsigned*>(vb)[tid];
+        const unsigned kc = reinterpret_cast<const unsigned*>(kb)[tid], vc = reinterpret_cast<const unsigned*>(vb)[v_c * LAPS_PAGE + v_off];
         const float ks = kv4_scale<0>(*k_scale), vs = kv4_scale<0>(*v_scale);
-        if (k_mine) k_tok[k_at] = kv4_eight(kc, ks);
-        if (v_mine) v_tok[v_at] = kv4_eight(vc, vs);
+        if (k_mine) put(kv4_eight(kc, ks), k_tok + k_at);
+        if (v_mine) put(kv4_eight(vc, vs), v_tok + v_at);
     }
 }
 
@@ -80,8 +92,13 @@ int laps_launch_kv4_move(bool scatter, int n_seq, int n_tokens, const int* cu, c
                          hipStream_t s) {
     if (n_tokens == 0) return LAPS_OK;
     const dim3 grid(n_tokens / LAPS_PAGE + 2 * n_seq, n_kv);
-    auto kern = hd == 128 ? (scatter ? kv4_move_kernel<128, true> : kv4_move_kernel<128, false>)
-                          : (scatter ? kv4_move_kernel<64, true> : kv4_move_kernel<64, false>);
+    const bool stream = (size_t)n_tokens * n_kv * hd * 2 * sizeof(bf16_t) > ((size_t)32 << 20);   // eight L2 caches of 4 MiB
+    auto pick = [&](auto HD) {
+        constexpr int D = decltype(HD)::value;
+        return scatter ? (stream ? kv4_move_kernel<D, true, true> : kv4_move_kernel<D, true, false>)
+                       : (stream ? kv4_move_kernel<D, false, true> : kv4_move_kernel<D, false, false>);
+    };
+    auto kern = hd == 128 ? pick(std::integral_constant<int, 128>{}) : pick(std::integral_constant<int, 64>{});
     hipLaunchKernelGGL(kern, grid, dim3(2 * hd), 0, s, cu, start_pos, page_table, static_cast<u32x4*>(k_tok),
                        static_cast<u32x4*>(v_tok), static_cast<unsigned char*>(k_pool), static_cast<unsigned char*>(v_pool), n_seq,
                        n_tokens, max_pages, n_kv, n_pool_pages);
