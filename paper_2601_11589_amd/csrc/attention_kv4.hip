@@ -26,7 +26,7 @@ namespace {
 
 constexpr int WAVES = 4;
 constexpr int STEP = 2 * LAPS_PAGE;   // keys a wave takes at a time
-constexpr int MAX_PARTS = 64;
+constexpr int MAX_PARTS = 96;         // a resident workgroup a place for 8 (sequence, kv head) pairs
 constexpr float MOST = 256.f;   // sum of eight weights above which the reference moves
 
 typedef unsigned char byte_t;
@@ -134,6 +134,9 @@ __global__ __launch_bounds__(WAVES * 64, NR == 1 ? 3 : 2) void attn_rows_kernel(
             ids = (id > 0 && id < n_pool_pages) ? id : 0;      // unset, or not a page of the pool
             asm volatile("" : "+v"(ids));   // waited for here: behind the join it would be waited for at every step, with all loads in flight
         };
+        // Up to 16 rows a sequence: keys are read once and past the caches, 2.3 GB 418 -> 378 us (6.0 TB/s; 280 MB that the memory-side cache
+        // held from the call before 52 -> 58).  More rows: other blocks of theirs read the same keys.
+        auto codes = [](const auto* from) { return NR == 1 ? __builtin_nontemporal_load(from) : *from; };
         auto load = [&](int n, Piece<HD>& x) {
             if ((n & 31) == 0) fetch_ids(n);
 #pragma unroll
@@ -142,16 +145,16 @@ __global__ __launch_bounds__(WAVES * 64, NR == 1 ? 3 : 2) void attn_rows_kernel(
                 const size_t at = ((size_t)page * n_kv + kvh) * BLOCK;
                 const byte_t *kb = k_pool + at, *vb = v_pool + at;
                 if constexpr (HD == 128) {
-                    const u32x4 w = reinterpret_cast<const u32x4*>(kb)[i * 4 + g];
+                    const u32x4 w = codes(reinterpret_cast<const u32x4*>(kb) + i * 4 + g);
 #pragma unroll
                     for (int kk = 0; kk < 4; ++kk) x.k[p][kk] = w[kk];
                 } else {
-                    const u32x2 w = reinterpret_cast<const u32x2*>(kb)[i * 4 + g];
+                    const u32x2 w = codes(reinterpret_cast<const u32x2*>(kb) + i * 4 + g);
                     x.k[p][0] = w.x;
                     x.k[p][1] = w.y;
                 }
                 x.ks[p] = reinterpret_cast<const unsigned*>(kb + CODES)[HD == 128 ? i : i >> 1];
-                x.v[p] = reinterpret_cast<const u32x4*>(vb)[v_chunk * 4 + g];
+                x.v[p] = codes(reinterpret_cast<const u32x4*>(vb) + v_chunk * 4 + g);
                 x.vs[p] = reinterpret_cast<const unsigned*>(vb + CODES)[v_group * 4 + g];
             }
         };
@@ -364,6 +367,7 @@ __global__ __launch_bounds__(8 * HD / 4) void attn_rows_merge_kernel(bf16_t* __r
                                                                      const int* __restrict__ prefix_len, int max_pages,
                                                                      int n_tokens, int n_q, int parts, int min_parts) {
     constexpr int LANES = HD / 4, GROUPS = 8;
+    static_assert(MAX_PARTS % GROUPS == 0 && MAX_PARTS <= 128, "two parts a lane, as many registers as a group has parts");
     __shared__ float weight[MAX_PARTS], l_all;
     __shared__ f32x4 red[GROUPS][LANES];
     const int head = blockIdx.x % n_q, seq = blockIdx.x / n_q, tid = threadIdx.x, c = tid % LANES, grp = tid / LANES;
@@ -374,19 +378,30 @@ __global__ __launch_bounds__(8 * HD / 4) void attn_rows_merge_kernel(bf16_t* __r
     if (used == 1) return;   // written by the attention kernel
     for (int t = blockIdx.y; t < r.L; t += gridDim.y) {
         const size_t at = ((size_t)(r.rs + t) * n_q + head) * parts;
-        const int run = (used + GROUPS - 1) / GROUPS, p0 = grp * run;   // at most 8 parts a group, all on their way before any is used
+        const int run = (used + GROUPS - 1) / GROUPS, p0 = grp * run;   // at most 12 parts a group, all on their way before any is used
         f32x4 v[MAX_PARTS / GROUPS];
 #pragma unroll
         for (int p = 0; p < MAX_PARTS / GROUPS; ++p)
             if (p < run) v[p] = reinterpret_cast<const f32x4*>(part_o + (at + (p0 + p < used ? p0 + p : used - 1)) * HD)[c];
-        if (tid < 64) {   // parts <= 64: one a lane
-            const float m = tid < used ? part_ml[(at + tid) * 2] : -INFINITY, l = tid < used ? part_ml[(at + tid) * 2 + 1] : 0.f;
-            float m_all = m;
+        if (tid < 64) {   // one wave: parts tid and tid + 64
+            float m[2], l[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int p = tid + 64 * k;
+                m[k] = p < used ? part_ml[(at + p) * 2] : -INFINITY;
+                l[k] = p < used ? part_ml[(at + p) * 2 + 1] : 0.f;
+            }
+            float m_all = fmaxf(m[0], m[1]);
 #pragma unroll
             for (int k = 32; k > 0; k >>= 1) m_all = fmaxf(m_all, __shfl_xor(m_all, k, 64));
-            const float f = __builtin_amdgcn_exp2f(m - (m_all == -INFINITY ? 0.f : m_all));
-            weight[tid] = f;
-            float sum = f * l;
+            const float m_sub = m_all == -INFINITY ? 0.f : m_all;
+            float sum = 0.f;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const float f = __builtin_amdgcn_exp2f(m[k] - m_sub);
+                if (tid + 64 * k < MAX_PARTS) weight[tid + 64 * k] = f;
+                sum += f * l[k];
+            }
 #pragma unroll
             for (int k = 32; k > 0; k >>= 1) sum += __shfl_xor(sum, k, 64);
             if (tid == 0) l_all = sum;
