@@ -518,14 +518,15 @@ Kv4RowsPlan laps_kv4_rows_plan(int n_seq, int n_tokens, int n_q, int n_kv, int m
     const long most = (1L << 20) / ((long)n_seq * n_kv);   // a grid of a million workgroups at most; they walk the blocks that are left
     blocks = blocks < most ? blocks : (most > 1 ? most : 1);
     const long rounds = ((long)max_pages * LAPS_PAGE + STEP * WAVES - 1) / (STEP * WAVES);   // of the longest sequence the table holds
-    // One resident workgroup a place on the chip (3 or 2 a unit) where the sequences are alike; twice as many parts at most where
-    // the table allows sequences long enough for the longest one to outlast the others and a part to be worth the merge.  32B,
-    // 64 tokens over 4096 keys each, 1 / 2 / 4 parts 47.8 / 51.3 / 58 us; over 512 to 8191 70.1 / 68.3 / 72, up to 3 by length 64.7;
-    // 96 over 16 to 1300 1 / 2 parts 20.5 / 26.2.
+    // One workgroup a place on the chip where the sequences are alike (3 or 2 are resident a unit; with 32 rows one is better than two
+    // with their merge); more parts where the table allows sequences long enough for the longest one to outlast the others.  32B, 64
+    // tokens over 4096 keys each, 1 / 2 / 4 parts 47.8 / 51.3 / 58 us; over 512 to 8191 70.1 / 68.3 / 72, up to 3 by length 64.7; 96 over
+    // 16 to 1300 1 / 2 parts 20.5 / 26.2.  16 times 8 tokens over 2048 keys 1 / 2 / 3 parts 25.9 / 25.2 / 29.0; 7B, 20 times 8 to 40 over
+    // 64 to 10000 1 / 2 parts 86 / 67.
     const long units = blocks * n_seq * n_kv, places = tiles == 1 ? 768 : 256;
-    auto within = [&](long n, long most) { return n < most ? n : most; };
+    auto within = [](long n, long most) { return n < most ? n : most; };
     const long min_parts = within(within(places / units, rounds), MAX_PARTS);
-    const long parts = within(within(2 * places / units, rounds / (tiles == 1 ? 16 : 8)), MAX_PARTS);
+    const long parts = within(within((tiles == 1 ? 1536 : 1024) / units, rounds / (tiles == 1 ? 16 : 12)), MAX_PARTS);
     return {tiles, (int)blocks, (int)(parts > min_parts ? parts : (min_parts > 1 ? min_parts : 1)), (int)(min_parts > 1 ? min_parts : 1)};
 }
 
