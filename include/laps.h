@@ -245,10 +245,16 @@ int laps_prefill_stack_static(laps_ctx* ctx, const laps_layer_weights* w, int32_
  * max_pages wide).  out[6] = { query rows per workgroup, bound on the (sequence, row block) work items,
  * key-range splits of an item at most (1 = none), fewest 64-key tiles a split is given, bytes of the work-item table, bytes of
  * the key-split partial results (0 if tables this narrow never split) }.
+ * laps_attention_kv4_plan_info: the same for 4-bit pools.  out[6] = { query rows per workgroup (16 or 32: the kernel for few rows;
+ * 128 or 256: blocks), row blocks of a sequence and kv head that have workgroups (blocks: bound on the work items), most and fewest
+ * parts of a sequence's keys (fewest as far as it has keys for them), workgroups of the persistent kernel (0 = a grid of blocks),
+ * workspace bytes }.
  * EINVAL on NULL or unsupported shapes. */
 int laps_gemm_plan_info(int32_t m, int32_t n, int32_t k, int32_t split_k, int32_t epilogue, int32_t* out);
 int laps_attn_plan_info(int32_t n_seq, int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
                         int32_t max_pages, int64_t* out);
+int laps_attention_kv4_plan_info(int32_t n_seq, int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                 int32_t max_pages, int64_t* out);
 
 /* ------------------------------------------------------------------ captured short buckets
  * Section 3.1: one graph per (length bucket L_b, depth B_d) with fixed operator topology and

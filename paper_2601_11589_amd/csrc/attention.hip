@@ -68,6 +68,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const bf16_t* __restri
                                                         const int* __restrict__ tile_start, int n_seq, int n_q,
                                                         int n_kv, float scale_log2e, int n_pool_pages, int n_tokens,
                                                         int max_items, const int4* __restrict__ bounds) {
+    static_assert(!SPLIT || !KV4, "key ranges of 4-bit pools are split in the kernel for few rows");
     constexpr int NTHR = NW * 64;
     constexpr int CPR = HD / 8;            // 16-byte chunks per K row
     constexpr int CPP = HD * 2;            // 16-byte chunks per page (K and V alike)
@@ -864,7 +865,7 @@ int launch_attn_persistent(const bf16_t* q, bf16_t* out, float* part, int n_wgs,
     return LAPS_OK;
 }
 
-template <int HD, bool KV4>
+template <int HD>
 int launch_attn_split(const bf16_t* q, bf16_t* out, float* part, const bf16_t* k_pool, const bf16_t* v_pool,
                       const int4* desc, const int* page_table,
                       int max_pages, const int* tile_start, int n_seq, int max_items, int n_split,
@@ -873,7 +874,7 @@ int launch_attn_split(const bf16_t* q, bf16_t* out, float* part, const bf16_t* k
     const size_t blocks = (size_t)max_items * n_kv * n_split;
     float* part_o = part;
     float* part_ml = part + blocks * 128 * HD;
-    hipLaunchKernelGGL((attn_kernel<HD, 4, true, false, false, KV4>), dim3(max_items, n_kv, n_split), dim3(256), 0, s, q, out, part_o, part_ml,
+    hipLaunchKernelGGL((attn_kernel<HD, 4, true, false>), dim3(max_items, n_kv, n_split), dim3(256), 0, s, q, out, part_o, part_ml,
                        k_pool, v_pool, desc, page_table, max_pages, tile_start, n_seq,
                        n_q, n_kv, scale_log2e, n_pool_pages, n_tokens, max_items, nullptr);
     LAPS_LAUNCH_CHECK();
@@ -896,9 +897,9 @@ static constexpr int kSplitTargetBlocks = 512;   // aim for two workgroups per c
 static constexpr int kSplitBelowBlocks = 256;    // launches with fewer un-split workgroups than this are split
 static constexpr int kSplitMax = 64;
 
-size_t laps_attn_partial_want(int n_seq, int n_tokens, int group, int n_kv, int hd, int max_pages) {
-    const size_t shares = (size_t)2 * LAPS_ATTN_MAX_WGS * LAPS_ATTN_LONG_ROWS * (hd + 2) * sizeof(float), parts = laps_attn_partial_bytes(hd, max_pages);
-    return laps_attn_persistent_wgs(n_seq, n_tokens, group, n_kv, hd, max_pages, shares) > 0 && shares > parts ? shares : parts;
+size_t laps_attn_shares_bytes(int n_seq, int n_tokens, int group, int n_kv, int hd, int max_pages) {
+    const size_t shares = (size_t)2 * LAPS_ATTN_MAX_WGS * LAPS_ATTN_LONG_ROWS * (hd + 2) * sizeof(float);
+    return laps_attn_persistent_wgs(n_seq, n_tokens, group, n_kv, hd, max_pages, shares) > 0 ? shares : 0;
 }
 size_t laps_attn_partial_bytes(int hd, int max_pages) {
     // page tables too narrow for two splits never take the split path (same test as attn_blocking)
@@ -1028,12 +1029,12 @@ static int launch_attention(const bf16_t* q, bf16_t* out, const bf16_t* k_pool, 
         return launch_attn_persistent<HD, KV4>(q, out, partial, n_wgs, bounds, k_pool, v_pool, desc, page_table, max_pages, tile_start,
                                                n_seq, max_items, n_q, n_kv, n_pool_pages, n_tokens, s);
     if (n_split > 1) {
-        if (!partial) {
-            laps_set_error("attention: key-split launch needs the partial-result workspace");
+        if (!partial || KV4) {   // launches this small over 4-bit pools have a kernel of their own
+            laps_set_error("attention: key-split launch needs the partial-result workspace and bf16 pools");
             return LAPS_EINVAL;
         }
-        return launch_attn_split<HD, KV4>(q, out, partial, k_pool, v_pool, desc, page_table, max_pages, tile_start, n_seq, max_items, n_split,
-                                          n_q, n_kv, n_pool_pages, n_tokens, s);
+        return launch_attn_split<HD>(q, out, partial, k_pool, v_pool, desc, page_table, max_pages, tile_start, n_seq, max_items, n_split, n_q,
+                                     n_kv, n_pool_pages, n_tokens, s);
     }
     // 128-row blocks that would be 256-row ones over more key tiles: summed up as those do, so that the width of the page table
     // does not show in the result (the sums of rounded probabilities are also the ones that match the second product:

@@ -26,6 +26,7 @@ namespace {
 
 constexpr int WAVES = 4;
 constexpr int STEP = 2 * LAPS_PAGE;   // keys a wave takes at a time
+static_assert(WAVES * STEP == LAPS_KV4_ROUND, "a step for every wave");
 constexpr int MAX_PARTS = 96;         // a resident workgroup a place for 8 (sequence, kv head) pairs
 constexpr float MOST = 256.f;   // sum of eight weights above which the reference moves
 
@@ -45,18 +46,8 @@ __device__ __forceinline__ bool seq_range(int seq, const int* cu, const int* seq
     return true;
 }
 
-// Parts of a sequence's keys, all of equal length: a share of `parts` of the longest range that the page table holds, but at least
-// min_parts of them as far as there is a step for every wave.
 __device__ __forceinline__ int part_steps(int kv_len, int max_pages, int parts, int min_parts, int* used) {
-    const int rounds = (kv_len + STEP * WAVES - 1) / (STEP * WAVES), most = (max_pages + 2 * WAVES - 1) / (2 * WAVES);
-    const int share = (most + parts - 1) / parts;
-    int n = (rounds + share - 1) / share;
-    n = n < min_parts ? min_parts : n;
-    n = n < parts ? n : parts;
-    n = n < rounds ? n : rounds;
-    const int each = (rounds + n - 1) / n;
-    *used = (rounds + each - 1) / each;
-    return each * WAVES;
+    return laps_kv4_part_rounds(kv_len, max_pages, parts, min_parts, used) * WAVES;
 }
 
 // One step's codes and scales as they come from the pools.
@@ -517,7 +508,7 @@ Kv4RowsPlan laps_kv4_rows_plan(int n_seq, int n_tokens, int n_q, int n_kv, int m
     long blocks = (rows + 16L * tiles * n_seq - 1) / (16L * tiles * n_seq);
     const long most = (1L << 20) / ((long)n_seq * n_kv);   // a grid of a million workgroups at most; they walk the blocks that are left
     blocks = blocks < most ? blocks : (most > 1 ? most : 1);
-    const long rounds = ((long)max_pages * LAPS_PAGE + STEP * WAVES - 1) / (STEP * WAVES);   // of the longest sequence the table holds
+    const long rounds = ((long)max_pages * LAPS_PAGE + LAPS_KV4_ROUND - 1) / LAPS_KV4_ROUND;   // of the longest sequence the table holds
     // One workgroup a place on the chip where the sequences are alike (3 or 2 are resident a unit; with 32 rows one is better than two
     // with their merge); more parts where the table allows sequences long enough for the longest one to outlast the others.  32B, 64
     // tokens over 4096 keys each, 1 / 2 / 4 parts 47.8 / 51.3 / 58 us; over 512 to 8191 70.1 / 68.3 / 72, up to 3 by length 64.7; 96 over

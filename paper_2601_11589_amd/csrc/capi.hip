@@ -620,23 +620,54 @@ extern "C" int laps_kv4_gather(laps_ctx* c, int32_t n_seq, int32_t n_tokens, con
 }
 
 // Workspace of the block kernels: lengths, work items, partial results.
-static WsLayout kv4_layout(const laps_model_cfg& c, int n_seq, int n_tokens, int max_pages) {
+static WsLayout kv4_layout(int n_seq, int n_tokens, int n_q, int n_kv, int hd, int max_pages) {
     WsLayout w = {};
-    const int group = c.n_q_heads / c.n_kv_heads;
+    const int group = n_q / n_kv;
     w.tile_start = align256((size_t)n_seq * 4);
     w.item_seq = w.tile_start + align256((size_t)(n_seq + 1) * 4);
     w.partial = w.item_seq + align256(laps_attn_item_table_bytes(n_tokens, n_seq, group));
-    w.total = w.partial + align256(laps_attn_partial_want(n_seq, n_tokens, group, c.n_kv_heads, c.head_dim, max_pages));
+    w.total = w.partial + align256(laps_attn_shares_bytes(n_seq, n_tokens, group, n_kv, hd, max_pages));
     return w;
 }
 
+static size_t kv4_workspace_bytes(int n_seq, int n_tokens, int n_q, int n_kv, int hd, int max_pages) {
+    if (n_seq < 1 || n_tokens < 1 || max_pages < 1 || max_pages > LAPS_KV4_MAX_PAGES || (long)n_seq * n_q > LAPS_KV4_MAX_SEQ_HEADS) return 0;
+    if (!laps_kv4_takes_rows(n_seq, n_tokens, n_q, n_kv)) return kv4_layout(n_seq, n_tokens, n_q, n_kv, hd, max_pages).total;
+    return align256(laps_kv4_rows_bytes(laps_kv4_rows_plan(n_seq, n_tokens, n_q, n_kv, max_pages), n_tokens, n_q, hd) + 1);
+}
+
 extern "C" size_t laps_attention_kv4_workspace_bytes(const laps_ctx* c, int32_t n_seq, int32_t n_tokens, int32_t max_pages) {
-    if (!c || n_seq < 1 || n_tokens < 1 || max_pages < 1 || max_pages > LAPS_KV4_MAX_PAGES || (long)n_seq * c->cfg.n_q_heads > LAPS_KV4_MAX_SEQ_HEADS)
-        return 0;
-    const laps_model_cfg& cf = c->cfg;
-    if (!laps_kv4_takes_rows(n_seq, n_tokens, cf.n_q_heads, cf.n_kv_heads)) return kv4_layout(cf, n_seq, n_tokens, max_pages).total;
-    const Kv4RowsPlan p = laps_kv4_rows_plan(n_seq, n_tokens, cf.n_q_heads, cf.n_kv_heads, max_pages);
-    return align256(laps_kv4_rows_bytes(p, n_tokens, cf.n_q_heads, cf.head_dim) + 1);
+    return c ? kv4_workspace_bytes(n_seq, n_tokens, c->cfg.n_q_heads, c->cfg.n_kv_heads, c->cfg.head_dim, max_pages) : 0;
+}
+
+extern "C" int laps_attention_kv4_plan_info(int32_t n_seq, int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                            int32_t max_pages, int64_t* out) {
+    size_t bytes = 0;
+    if (out && n_q_heads >= 1 && n_kv_heads >= 1 && n_q_heads % n_kv_heads == 0 && (head_dim == 64 || head_dim == 128))
+        bytes = kv4_workspace_bytes(n_seq, n_tokens, n_q_heads, n_kv_heads, head_dim, max_pages);
+    if (bytes == 0) {
+        laps_set_error("attention_kv4_plan_info: NULL output or unsupported shape");
+        return LAPS_EINVAL;
+    }
+    out[5] = (int64_t)bytes;
+    if (laps_kv4_takes_rows(n_seq, n_tokens, n_q_heads, n_kv_heads)) {
+        const Kv4RowsPlan p = laps_kv4_rows_plan(n_seq, n_tokens, n_q_heads, n_kv_heads, max_pages);
+        out[0] = 16 * p.row_tiles;
+        out[1] = p.row_blocks;
+        out[2] = p.parts;
+        out[3] = p.min_parts;
+        out[4] = 0;
+        return LAPS_OK;
+    }
+    int rows = 0, items = 0, split = 0, min_tiles = 0;
+    const int group = n_q_heads / n_kv_heads;
+    const WsLayout L = kv4_layout(n_seq, n_tokens, n_q_heads, n_kv_heads, head_dim, max_pages);
+    laps_attn_plan(n_seq, n_tokens, group, n_kv_heads, max_pages, &rows, &items, &split, &min_tiles);
+    out[0] = rows;
+    out[1] = items;
+    out[2] = out[3] = split;
+    out[4] = laps_attn_persistent_wgs(n_seq, n_tokens, group, n_kv_heads, head_dim, max_pages, L.total - L.partial);
+    return LAPS_OK;
 }
 
 extern "C" int laps_attention_kv4(laps_ctx* c, int32_t n_seq, int32_t n_tokens, const int32_t* cu, const int32_t* seq_len,
@@ -670,7 +701,7 @@ extern "C" int laps_attention_kv4(laps_ctx* c, int32_t n_seq, int32_t n_tokens, 
         const Kv4RowsPlan p = laps_kv4_rows_plan(n_seq, n_tokens, a.n_q, a.n_kv, max_pages);
         return laps_launch_kv4_rows(a, p, p.parts > 1 ? static_cast<float*>(ws) : nullptr, s);
     }
-    const WsLayout L = kv4_layout(cf, n_seq, n_tokens, max_pages);
+    const WsLayout L = kv4_layout(n_seq, n_tokens, cf.n_q_heads, cf.n_kv_heads, cf.head_dim, max_pages);
     unsigned char* w8 = static_cast<unsigned char*>(ws);
     const BatchDesc b{n_seq, n_tokens, cu, seq_len, prefix_len, pt, max_pages};
     LAPS_TRY(laps_launch_begin(begin_args(c, b, w8, L), s));

@@ -306,14 +306,32 @@ static __device__ __forceinline__ void laps_dev_attn_bounds(const int* __restric
     }
 }
 
+// Parts of a sequence's keys in the attention of few query rows over the 4-bit cache, all of the returned number of rounds of
+// LAPS_KV4_ROUND keys (the last one what is left): a share of `parts` of the longest range that the page table holds, but at least
+// min_parts of them as far as there are rounds.  From the sequence's own length and the launch's shape alone, so that the bits of a
+// request do not depend on the lengths it is batched with.
+constexpr int LAPS_KV4_ROUND = 128;
+static __host__ __device__ inline int laps_kv4_part_rounds(int kv_len, int max_pages, int parts, int min_parts, int* used) {
+    constexpr int PAGES = LAPS_KV4_ROUND / LAPS_PAGE;
+    const int rounds = (kv_len + LAPS_KV4_ROUND - 1) / LAPS_KV4_ROUND, most = (max_pages + PAGES - 1) / PAGES;
+    const int share = (most + parts - 1) / parts;
+    int n = (rounds + share - 1) / share;
+    n = n < min_parts ? min_parts : n;
+    n = n < parts ? n : parts;
+    n = n < rounds ? n : rounds;
+    const int each = (rounds + n - 1) / n;
+    *used = (rounds + each - 1) / each;
+    return each;
+}
+
 // ----------------------------------------------------------------------------- attention
 // The work-item table is made with the blocking of the same (n_seq, n_tokens, max_pages) (laps_attn_plan).
 // `partial` (partial_bytes >= laps_attn_partial_bytes, 16-byte aligned) receives per-split results when the launch shape
 // calls for splitting the key range; it may be NULL only if max_pages * 16 < 512.  partial_bytes must be that of the table's shares.
 // tile_start: n_seq + 1 ints; item_seq: laps_attn_item_table_bytes (sequence of every row-block work item).
 size_t laps_attn_partial_bytes(int hd, int max_pages);   // 0 when page tables this narrow never split
-// For a launch of its own: as much as it can use.
-size_t laps_attn_partial_want(int n_seq, int n_tokens, int group, int n_kv, int hd, int max_pages);
+// Bytes that the shares of a persistent launch of its own can use, 0 if the shape has none.
+size_t laps_attn_shares_bytes(int n_seq, int n_tokens, int group, int n_kv, int hd, int max_pages);
 // Work-item table: item_seq, then the cost prefix sums and the bounds of the persistent kernel and the items' descriptions.
 size_t laps_attn_item_table_bytes(int max_tokens, int max_seqs, int group);
 void laps_attn_item_tables(int* item_seq, int n_tokens, int n_seq, int group, int** pre, int4** bounds, int4** desc);

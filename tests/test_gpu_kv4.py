@@ -189,6 +189,67 @@ def test_head_layouts(heads):
     b.ctx.close()
 
 
+# Batches large enough for the kernels of 128 and 256 rows, 64 query heads over 8: (new, prefix, spare pages, rows a workgroup, shares)
+BLOCKS = {
+    "shares": ([300, 40, 260], [1500, 200, 0], 2, 256, True),
+    "shares_wide_table": ([520, 1, 0, 77], [0, 3000, 5, 1100], 300, 256, True),
+    "grid_of_256": ([400, 300], [100, 0], 0, 256, False),
+    "one_prompt": ([600], [0], 2, 256, False),
+    "halves": ([48] * 11 + [47], [70, 0, 150, 3, 64, 16, 15, 17, 100, 31, 1, 128], 0, 128, False),
+    "one_tile": ([9] * 70 + [1, 0], [7] * 72, 0, 128, False),
+    "plain": ([16] * 39 + [3], [30, 0, 200, 64] * 10, 0, 128, False),
+}
+
+
+def big_cfg(hd):
+    return inputs.ModelCfg(256, 64, 8, hd, 512, 1)
+
+
+def plan(b):
+    out = (C.c_int64 * 6)()
+    assert api.lib().laps_attention_kv4_plan_info(C.c_int32(len(b.new)), C.c_int32(len(b.q)), C.c_int32(b.cfg.n_q_heads),
+                                                  C.c_int32(b.cfg.n_kv_heads), C.c_int32(b.cfg.head_dim), C.c_int32(b.table.shape[1]), out) == 0
+    return list(out)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("name", sorted(BLOCKS))
+def test_blocks_match_the_definition(name, hd):
+    new, pre, spare, rows, shares = BLOCKS[name]
+    b = Batch(big_cfg(hd), new, pre, spare=spare, seed=hd).write()
+    p = plan(b)
+    assert p[0] == rows and (p[4] > 0) == shares, p
+    b.check(b.attend())
+    b.ctx.close()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("name,at", [("shares", 1700), ("shares", 1499), ("shares", 3), ("grid_of_256", 330), ("halves", 70), ("plain", 33)])
+def test_a_nan_in_blocks_reaches_the_rows_that_see_it(name, at, hd):
+    new, pre, spare, rows, _ = BLOCKS[name]
+    for which in ("v", "k"):
+        b = Batch(big_cfg(hd), new, pre, spare=spare, seed=at)
+        (b.v if which == "v" else b.k)[at, 1, 37] = math.nan
+        b.write()
+        assert plan(b)[0] == rows
+        want = b.oracle()
+        assert np.isnan(want[0]).any() and not np.isnan(want[0]).all()
+        b.check(b.attend(), want)
+        b.ctx.close()
+
+
+@pytest.mark.parametrize("name,rows", [("shares", 256), ("halves", 256), ("plain", 128)])     # by all rows, padding among them
+def test_rows_without_a_token_stay_in_blocks(name, rows):
+    new, pre, spare, _, _ = BLOCKS[name]
+    b = Batch(big_cfg(128), new, pre, spare=spare, pad=[(3 * i) % 5 for i in range(len(new))]).write()
+    assert plan(b)[0] == rows
+    out = torch.full(b.q.shape, 7.5, dtype=torch.bfloat16, device="cuda")
+    live = b.check(b.attend(out))
+    rest = np.setdiff1d(np.arange(len(b.q)), live)
+    assert len(rest) > 0 and (out[torch.from_numpy(rest).cuda()] == 7.5).all()
+    b.ctx.close()
+
+
 def test_many_sequences():
     g = np.random.default_rng(8)
     b = Batch(inputs.tiny_cfg(1), g.integers(0, 3, 700), g.integers(0, 90, 700)).write()
@@ -336,7 +397,7 @@ def test_prefill_cache_goes_on_in_four_bits():
 
 
 # ------------------------------------------------------------------------------------------------ streams, graphs, refusals
-@pytest.mark.parametrize("new,pre", [([1, 1, 1], [700, 20, 3000]), ([40, 30], [500, 900]), ([300], [100])])
+@pytest.mark.parametrize("new,pre", [([1, 1, 1], [700, 20, 3000]), ([40, 30], [500, 900]), ([1300], [100])])
 def test_captured_steps_replay_with_new_contents(new, pre):
     """Two graphs of one step each (write, attend), replayed in turns with other tokens, lengths and queries in between eager calls."""
     b = Batch(inputs.qwen7b_cfg(1), new, pre).write("cached")

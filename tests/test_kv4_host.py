@@ -2,6 +2,9 @@
 and their binding refuse."""
 import ctypes as C
 import math
+import os
+import random
+import subprocess
 
 import numpy as np
 import pytest
@@ -86,3 +89,77 @@ def test_binding_refuses_other_tensors(t):
 def test_model_shapes_have_whole_groups():
     for f in (inputs.tiny_cfg, inputs.qwen7b_cfg, inputs.qwen14b_cfg, inputs.qwen32b_cfg):
         assert f(1).head_dim % O.GROUP == 0
+
+
+# ------------------------------------------------------------------------------------------------ launch plans
+def plan(n_seq, n_tokens, heads, pages):
+    out = (C.c_int64 * 6)()
+    rc = api.lib().laps_attention_kv4_plan_info(C.c_int32(n_seq), C.c_int32(n_tokens), *(C.c_int32(h) for h in heads), C.c_int32(pages), out)
+    return dict(zip(("rows", "blocks", "parts", "min_parts", "shares", "bytes"), list(out))) if rc == 0 else None
+
+
+HEADS = [(4, 2, 64), (28, 4, 128), (40, 8, 128), (64, 8, 64), (8, 8, 128), (71, 1, 64)]
+
+
+def shapes(n, seed):
+    g = random.Random(seed)
+    for _ in range(n):
+        n_seq = int(math.exp(g.uniform(0, math.log(3000))))
+        tokens = max(1, int(n_seq * math.exp(g.uniform(math.log(0.5), math.log(300)))))
+        yield n_seq, tokens, g.choice(HEADS), int(math.exp(g.uniform(0, math.log(1 << 17))))
+
+
+def test_plans_of_few_rows_hold_what_their_kernel_assumes():
+    for n_seq, tokens, heads, pages in shapes(4000, 1):
+        p, (n_q, n_kv, hd) = plan(n_seq, tokens, heads, pages), heads
+        what = (n_seq, tokens, heads, pages, p)
+        mean = tokens * (n_q // n_kv) / n_seq
+        if p["rows"] > 32:      # blocks: never a split key range, whose kernel reads bf16 pools only
+            assert p["rows"] in (128, 256) and p["parts"] == 1 and mean > 16, what
+            assert p["shares"] == 0 or p["rows"] == 256, what
+            assert p["bytes"] >= p["shares"] * 2 * 256 * (hd + 2) * 4 + p["blocks"] * 32, what
+            continue
+        assert p["rows"] == (16 if mean <= 16 else 32) and 1 <= p["min_parts"] <= p["parts"] <= 96, what
+        assert p["blocks"] * n_seq * n_kv <= max(1 << 20, n_seq * n_kv), what
+        assert p["blocks"] * p["rows"] * n_seq >= tokens * (n_q // n_kv) or p["blocks"] * n_seq * n_kv > (1 << 19), what
+        assert p["bytes"] >= (tokens * n_q * p["parts"] * (hd + 2) * 4 if p["parts"] > 1 else 1), what
+        assert p["bytes"] <= 64 << 20, what      # what lies between the kernels stays small
+
+
+def test_plans_refuse():
+    assert plan(1, 1, (40, 8, 128), 10) is not None
+    for bad in ((0, 1, (40, 8, 128), 10), (1, 0, (40, 8, 128), 10), (1, 1, (40, 8, 128), 0), (1, 1, (40, 8, 96), 10), (1, 1, (40, 7, 128), 10),
+                (1, 1, (40, 8, 128), (1 << 26) + 1), (1 << 15, 1 << 15, (40, 8, 128), 10)):
+        assert plan(*bad) is None, bad
+
+
+@pytest.fixture(scope="module")
+def parts_driver(tmp_path_factory, repo_root):
+    exe = str(tmp_path_factory.mktemp("parts") / "kv4_parts")
+    build = subprocess.run(["/opt/rocm/bin/hipcc", "-x", "c++", "-std=c++17", "-O1", "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include",
+                            os.path.join(repo_root, "tests", "kv4_parts_driver.cpp"), "-o", exe], capture_output=True, text=True)
+    assert build.returncode == 0, build.stderr
+
+    def run(lines):
+        r = subprocess.run([exe], input="\n".join(" ".join(map(str, x)) for x in lines) + "\n", capture_output=True, text=True, timeout=120)
+        assert r.returncode == 0, r.stderr
+        return [tuple(map(int, x.split())) for x in r.stdout.splitlines()]
+
+    return run
+
+
+def test_parts_cover_the_keys(parts_driver):
+    g = random.Random(2)
+    asked = []
+    for n_seq, tokens, heads, pages in shapes(600, 3):
+        p = plan(n_seq, tokens, heads, pages)
+        if p["rows"] <= 32:
+            for kv_len in (1, pages * 16, g.randint(1, pages * 16), min(pages * 16, 128), min(pages * 16, 129)):
+                asked.append((kv_len, pages, p["parts"], p["min_parts"]))
+    assert len(asked) > 1000
+    for (kv_len, pages, parts, least), (each, used) in zip(asked, parts_driver(asked), strict=True):
+        what = (kv_len, pages, parts, least, each, used)
+        rounds = -(-kv_len // 128)
+        assert 1 <= used <= parts and each >= 1 and (used - 1) * each < rounds <= used * each, what
+        assert used == rounds or used >= min(least, rounds) * 0.5, what      # equal lengths may need fewer parts than asked for
+        assert each <= max(-(-rounds // least), -(-(-(-pages // 8)) // parts)), what   # none longer than its share of the table
