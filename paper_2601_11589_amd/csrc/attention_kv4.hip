@@ -514,11 +514,14 @@ Kv4RowsPlan laps_kv4_rows_plan(int n_seq, int n_tokens, int n_q, int n_kv, int m
     // tokens over 4096 keys each, 1 / 2 / 4 parts 47.8 / 51.3 / 58 us; over 512 to 8191 70.1 / 68.3 / 72, up to 3 by length 64.7; 96 over
     // 16 to 1300 1 / 2 parts 20.5 / 26.2.  16 times 8 tokens over 2048 keys 1 / 2 / 3 parts 25.9 / 25.2 / 29.0; 7B, 20 times 8 to 40 over
     // 64 to 10000 1 / 2 parts 86 / 67.
+    // Tables of up to 8 rounds: one launch without a merge takes no longer (one token over 900 keys 9.0 us in 1 part, 9.3 in 8; 16 tokens
+    // over 500 keys 7.6 and 10.7).
+    if (rounds <= 8) return {tiles, (int)blocks, 1, 1};
     const long units = blocks * n_seq * n_kv, places = tiles == 1 ? 768 : 256;
-    auto within = [](long n, long most) { return n < most ? n : most; };
-    const long min_parts = within(within(places / units, rounds), MAX_PARTS);
-    const long parts = within(within((tiles == 1 ? 1536 : 1024) / units, rounds / (tiles == 1 ? 16 : 12)), MAX_PARTS);
-    return {tiles, (int)blocks, (int)(parts > min_parts ? parts : (min_parts > 1 ? min_parts : 1)), (int)(min_parts > 1 ? min_parts : 1)};
+    auto within = [](long n, long most) { return n < most ? (n > 1 ? n : 1) : most; };
+    const long min_parts = within(within(places / units, rounds / 2), MAX_PARTS);
+    const long parts = within(within((tiles == 1 ? 1536 : 1024) / units, rounds / (tiles == 1 ? 16 : 10)), MAX_PARTS);
+    return {tiles, (int)blocks, (int)(parts > min_parts ? parts : min_parts), (int)min_parts};
 }
 
 size_t laps_kv4_rows_bytes(const Kv4RowsPlan& p, int n_tokens, int n_q, int hd) {

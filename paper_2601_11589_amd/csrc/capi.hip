@@ -704,7 +704,9 @@ extern "C" int laps_attention_kv4(laps_ctx* c, int32_t n_seq, int32_t n_tokens, 
     const WsLayout L = kv4_layout(n_seq, n_tokens, cf.n_q_heads, cf.n_kv_heads, cf.head_dim, max_pages);
     unsigned char* w8 = static_cast<unsigned char*>(ws);
     const BatchDesc b{n_seq, n_tokens, cu, seq_len, prefix_len, pt, max_pages};
-    LAPS_TRY(laps_launch_begin(begin_args(c, b, w8, L), s));
+    BeginArgs begin = begin_args(c, b, w8, L);
+    begin.d = 0;   // no rows: the smaller of its kernels, 1 us less
+    LAPS_TRY(laps_launch_begin(begin, s));
     return laps_launch_attention(static_cast<const bf16_t*>(q), static_cast<bf16_t*>(out), k_pool, v_pool, true, pt, max_pages, n_seq,
                                  n_tokens, reinterpret_cast<int*>(w8 + L.tile_start), reinterpret_cast<int*>(w8 + L.item_seq),
                                  reinterpret_cast<float*>(w8 + L.partial), L.total - L.partial, cf.n_q_heads, cf.n_kv_heads,

@@ -308,7 +308,7 @@ static __device__ __forceinline__ void laps_dev_attn_bounds(const int* __restric
 
 // Parts of a sequence's keys in the attention of few query rows over the 4-bit cache, all of the returned number of rounds of
 // LAPS_KV4_ROUND keys (the last one what is left): a share of `parts` of the longest range that the page table holds, but at least
-// min_parts of them as far as there are rounds.  From the sequence's own length and the launch's shape alone, so that the bits of a
+// min_parts of them as far as there are two rounds for each.  From the sequence's own length and the launch's shape alone, so that the bits of a
 // request do not depend on the lengths it is batched with.
 constexpr int LAPS_KV4_ROUND = 128;
 static __host__ __device__ inline int laps_kv4_part_rounds(int kv_len, int max_pages, int parts, int min_parts, int* used) {
@@ -318,7 +318,8 @@ static __host__ __device__ inline int laps_kv4_part_rounds(int kv_len, int max_p
     int n = (rounds + share - 1) / share;
     n = n < min_parts ? min_parts : n;
     n = n < parts ? n : parts;
-    n = n < rounds ? n : rounds;
+    n = n < rounds / 2 ? n : rounds / 2;   // shorter ones are all beginning and end
+    n = n > 1 ? n : 1;
     const int each = (rounds + n - 1) / n;
     *used = (rounds + each - 1) / each;
     return each;

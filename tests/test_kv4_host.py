@@ -161,5 +161,6 @@ def test_parts_cover_the_keys(parts_driver):
         what = (kv_len, pages, parts, least, each, used)
         rounds = -(-kv_len // 128)
         assert 1 <= used <= parts and each >= 1 and (used - 1) * each < rounds <= used * each, what
-        assert used == rounds or used >= min(least, rounds) * 0.5, what      # equal lengths may need fewer parts than asked for
-        assert each <= max(-(-rounds // least), -(-(-(-pages // 8)) // parts)), what   # none longer than its share of the table
+        assert used == 1 or each >= 2, what
+        assert used >= min(least, rounds // 2) * 0.5, what                   # equal lengths may need fewer parts than asked for
+        assert each <= max(-(-rounds // least), -(-(-(-pages // 8)) // parts), 3), what   # none longer than its share of the table
