@@ -446,6 +446,30 @@ def test_two_streams_at_once():
     ctx.close()
 
 
+@pytest.mark.parametrize("n_new", [1, 3, 400])
+def test_pages_that_sequences_share(n_new):
+    """Two sequences over one prefix's pages, one of them with a page of it twice; written and read back on another stream."""
+    cfg = inputs.qwen7b_cfg(1)
+    b = Batch(cfg, [n_new, n_new], [320, 320])
+    b.table[1, :20] = b.table[0, :20]
+    b.table[1, 7] = b.table[1, 3]
+    side = torch.cuda.Stream()
+    at = np.concatenate([np.arange(320 + n_new), b.first[1] + np.arange(320, 320 + n_new)])   # the prefix once
+    cu, start, table = dev([0, 320 + n_new, 320 + 2 * n_new]), dev([0, 320]), dev(b.table)
+    b.ctx.laps_kv4_scatter(cu, start, table, b.k[at].cuda(), b.v[at].cuda(), b.k4, b.v4, stream=side)
+    rk, rv = b.ctx.laps_kv4_gather(dev([0, 320 + n_new, 640 + 2 * n_new]), dev([0, 0]), table, b.k4, b.v4, 640 + 2 * n_new, stream=side)
+    got = b.attend(stream=side)
+    side.synchronize()
+    seen = np.arange(320 + n_new)
+    seen[7 * 16:8 * 16] = np.arange(3 * 16, 4 * 16)
+    seen = np.concatenate([np.arange(320 + n_new), np.where(seen < 320, seen, b.first[1] + seen)])
+    for x, r in ((b.k, rk), (b.v, rv)):
+        x.copy_(x[seen].clone())
+        assert np.array_equal(wide(r), O.value(*O.quantise(wide(x))))
+    b.check(got)
+    b.ctx.close()
+
+
 def test_results_repeat_and_do_not_depend_on_the_batch():
     cfg = inputs.qwen14b_cfg(1)
     b = Batch(cfg, [1] * 5, [3000, 10, 700, 64, 1999]).write()
