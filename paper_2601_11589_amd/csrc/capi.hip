@@ -865,6 +865,7 @@ extern "C" int laps_attn_plan_info(int32_t n_seq, int32_t n_tokens, int32_t n_q_
 struct laps_graph {
     laps_ctx* ctx;
     int len_bucket, depth, max_pages, n_layers;
+    int pool_pages;        // the context's at the capture: its pools are the ones captured, later calls may be given others
     unsigned char* block;  // one device allocation holding everything below
     size_t block_bytes;
     float *x_in, *x_out;
@@ -892,7 +893,7 @@ static int graph_stage_launch(laps_graph* g, int n_real, const int* seq_len, con
     a.depth = g->depth;
     a.len_bucket = g->len_bucket;
     a.max_pages = g->max_pages;
-    a.n_pool_pages = g->ctx->pool_pages;
+    a.n_pool_pages = g->pool_pages;
     a.group = cf.n_q_heads / cf.n_kv_heads;
     laps_attn_plan(g->depth, M, a.group, cf.n_kv_heads, g->max_pages, &a.rows_per_wg, &a.max_items, &a.n_split, &a.min_tiles);
     a.n_kv = cf.n_kv_heads;
@@ -945,6 +946,7 @@ extern "C" int laps_graph_capture(laps_ctx* c, const laps_layer_weights* w, int3
     g->depth = depth;
     g->max_pages = max_pages;
     g->n_layers = nl;
+    g->pool_pages = c->pool_pages;
     const size_t M = (size_t)len_bucket * depth, d = c->cfg.hidden;
     const size_t ws_bytes = ws_layout(c->cfg, (int)M, depth, max_pages).total;
     size_t o = 0;
