@@ -153,6 +153,10 @@ void laps_ctx_destroy(laps_ctx* ctx);
  * the pools.  0 switches the check off (the default: the library does not know the pools' size).  A
  * graph keeps the value that was set when it was captured.  EINVAL on NULL or a negative count. */
 int laps_ctx_set_pool_pages(laps_ctx* ctx, int32_t n_pages);
+/* The same for the 4-bit pools of the laps_kv4_* and laps_attention_kv4 calls that follow, whose size may be another one.  0
+ * (the default): as laps_ctx_set_pool_pages says.  Threads that share a context and differ in their pools' size keep others out between
+ * setting a count and the call it is for. */
+int laps_ctx_set_kv4_pool_pages(laps_ctx* ctx, int32_t n_pages);
 /* Bytes of scratch laps_prefill_layer / laps_prefill_stack need for up to max_tokens rows
  * (padded rows count) and max_seqs sequences.  0 on bad arguments. */
 size_t laps_workspace_bytes(const laps_ctx* ctx, int32_t max_tokens, int32_t max_seqs);

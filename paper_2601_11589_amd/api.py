@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import threading
 
 import numpy as np
 import torch
@@ -88,6 +89,7 @@ def lib():
         L.laps_graph_destroy.argtypes = [C.c_void_p]
         p, i = C.c_void_p, C.c_int32
         L.laps_kv4_block_bytes.argtypes = [i]
+        L.laps_ctx_set_kv4_pool_pages.argtypes = [p, i]
         L.laps_kv4_scatter.argtypes = L.laps_kv4_gather.argtypes = [p, i, i, p, p, p, i, p, p, p, p, p]
         L.laps_attention_kv4_workspace_bytes.argtypes = [p, i, i, i]
         L.laps_attention_kv4.argtypes = [p, i, i, p, p, p, p, i, p, p, p, p, p, C.c_size_t, p]
@@ -383,6 +385,7 @@ class LapsCtx:
         _check(lib().laps_ctx_create(C.byref(self._c), C.c_int32(max_positions), C.byref(self._h)))
         self._ws = None
         self._kv4_block = lib().laps_kv4_block_bytes(cfg.head_dim)
+        self._kv4_lock = threading.Lock()
 
     def close(self):
         if self._h:
@@ -483,12 +486,18 @@ class LapsCtx:
                 _expect("page_table", page_table, torch.int32, (n_seq, width), device),
                 _expect("k4_pool", k4_pool, torch.uint8, pools, device), _expect("v4_pool", v4_pool, torch.uint8, pools, device))
 
-    def _kv4_stream(self, stream, k4_pool, device):
-        self._guard_pools(k4_pool)
+    def _kv4_stream(self, stream, device):
         if stream is None:   # the address alone where torch hands it out: 1 us less than with a stream object around it
             return _raw_stream(device) if _raw_stream else torch.cuda.current_stream(device).cuda_stream
         _after_current(stream)
         return stream.cuda_stream
+
+    def _kv4_launch(self, call, k4_pool, *args):
+        """One call on pools of k4_pool's pages.  That count lies in the context (and is the 4-bit pools' alone): no other thread's may
+        come between it and the call."""
+        with self._kv4_lock:
+            _check(lib().laps_ctx_set_kv4_pool_pages(self._h, k4_pool.shape[0]))
+            _check(call(self._h, *args))
 
     def laps_kv4_scatter(self, cu, start_pos, page_table, k_src, v_src, k4_pool, v4_pool, stream=None):
         """Quantises token-major bf16 K/V [n_tokens, n_kv_heads, head_dim] into 4-bit pools (new_kv4_pools)."""
@@ -496,8 +505,8 @@ class LapsCtx:
         shape = (k_src.shape[0], self.cfg.n_kv_heads, self.cfg.head_dim)
         start_p = _expect("start_pos", start_pos, torch.int32, (n_seq,), device)
         src_k, src_v = _expect("k_src", k_src, torch.bfloat16, shape, device), _expect("v_src", v_src, torch.bfloat16, shape, device)
-        s = self._kv4_stream(stream, k4_pool, device)
-        _check(lib().laps_kv4_scatter(self._h, n_seq, shape[0], cu_p, start_p, table_p, width, src_k, src_v, k_p, v_p, s))
+        s = self._kv4_stream(stream, device)
+        self._kv4_launch(lib().laps_kv4_scatter, k4_pool, n_seq, shape[0], cu_p, start_p, table_p, width, src_k, src_v, k_p, v_p, s)
 
     def laps_kv4_gather(self, cu, start_pos, page_table, k4_pool, v4_pool, n_tokens, k_out=None, v_out=None, stream=None):
         """Reads token-major bf16 K/V back from 4-bit pools, into k_out / v_out if given.  Rows without a page keep what they
@@ -508,8 +517,8 @@ class LapsCtx:
         k = torch.empty(shape, dtype=torch.bfloat16, device=k4_pool.device) if k_out is None else k_out
         v = torch.empty(shape, dtype=torch.bfloat16, device=k4_pool.device) if v_out is None else v_out
         dst_k, dst_v = _expect("k_out", k, torch.bfloat16, shape, device), _expect("v_out", v, torch.bfloat16, shape, device)
-        s = self._kv4_stream(stream, k4_pool, device)
-        _check(lib().laps_kv4_gather(self._h, n_seq, n_tokens, cu_p, start_p, table_p, width, k_p, v_p, dst_k, dst_v, s))
+        s = self._kv4_stream(stream, device)
+        self._kv4_launch(lib().laps_kv4_gather, k4_pool, n_seq, n_tokens, cu_p, start_p, table_p, width, k_p, v_p, dst_k, dst_v, s)
         if stream is not None:
             _held_by(stream, *(t for t, given in ((k, k_out), (v, v_out)) if given is None))
         return k, v
@@ -529,9 +538,9 @@ class LapsCtx:
         y_p = _expect("out", y, torch.bfloat16, shape, device)
         need = lib().laps_attention_kv4_workspace_bytes(self._h, n_seq, shape[0], width)
         ws = torch.empty(need or 256, dtype=torch.uint8, device=q.device)
-        s = self._kv4_stream(stream, k4_pool, device)
-        _check(lib().laps_attention_kv4(self._h, n_seq, shape[0], cu_p, len_p, pre_p, table_p, width, k_p, v_p, q_p, y_p,
-                                        ws.data_ptr(), need, s))
+        s = self._kv4_stream(stream, device)
+        self._kv4_launch(lib().laps_attention_kv4, k4_pool, n_seq, shape[0], cu_p, len_p, pre_p, table_p, width, k_p, v_p, q_p, y_p,
+                         ws.data_ptr(), need, s)
         if stream is not None:
             _held_by(stream, ws, *((y,) if out is None else ()))
         return y

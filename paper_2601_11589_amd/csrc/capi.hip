@@ -64,6 +64,7 @@ struct laps_ctx {
     int device;
     int max_pos;
     int pool_pages;  // page ids must be below this (INT_MAX: unknown, not checked)
+    int kv4_pages;   // the same of 4-bit pools (0: as pool_pages)
     float2* rope;  // [max_pos][hd/2] (cos, sin)
     unsigned char* static_ws;  // this device's copy of the static scratch array (resolved at creation)
     // timing
@@ -182,6 +183,7 @@ extern "C" int laps_ctx_create(const laps_model_cfg* cfg, int32_t max_positions,
     c->cfg = *cfg;
     c->max_pos = max_positions;
     c->pool_pages = INT_MAX;
+    c->kv4_pages = 0;
     c->rope = nullptr;
     c->static_ws = nullptr;
     c->prof_on = false;
@@ -228,6 +230,15 @@ extern "C" int laps_ctx_set_pool_pages(laps_ctx* c, int32_t n_pages) {
     c->pool_pages = n_pages == 0 ? INT_MAX : n_pages;
     return LAPS_OK;
 }
+extern "C" int laps_ctx_set_kv4_pool_pages(laps_ctx* c, int32_t n_pages) {
+    if (!c || n_pages < 0) {
+        laps_set_error("ctx_set_kv4_pool_pages: NULL context or negative page count");
+        return LAPS_EINVAL;
+    }
+    c->kv4_pages = n_pages;
+    return LAPS_OK;
+}
+static int kv4_pool_pages(const laps_ctx* c) { return c->kv4_pages ? c->kv4_pages : c->pool_pages; }
 
 extern "C" size_t laps_workspace_bytes(const laps_ctx* c, int32_t max_tokens, int32_t max_seqs) {
     if (!c || max_tokens < 1 || max_seqs < 1) return 0;
@@ -602,7 +613,7 @@ static int kv4_move(bool scatter, laps_ctx* c, int n_seq, int n_tokens, const in
     }
     LAPS_TRY(check_current_device(c, "kv4 move"));
     return laps_launch_kv4_move(scatter, n_seq, n_tokens, cu, start_pos, pt, max_pages, k_tok, v_tok, k_pool, v_pool,
-                                c->cfg.n_kv_heads, c->cfg.head_dim, c->pool_pages, static_cast<hipStream_t>(stream));
+                                c->cfg.n_kv_heads, c->cfg.head_dim, kv4_pool_pages(c), static_cast<hipStream_t>(stream));
 }
 
 extern "C" int laps_kv4_scatter(laps_ctx* c, int32_t n_seq, int32_t n_tokens, const int32_t* cu, const int32_t* start_pos,
@@ -697,7 +708,7 @@ extern "C" int laps_attention_kv4(laps_ctx* c, int32_t n_seq, int32_t n_tokens, 
     if (laps_kv4_takes_rows(n_seq, n_tokens, cf.n_q_heads, cf.n_kv_heads)) {
         const Kv4Attn a = {static_cast<const bf16_t*>(q), static_cast<bf16_t*>(out), static_cast<const unsigned char*>(k_pool),
                            static_cast<const unsigned char*>(v_pool), cu, seq_len, prefix_len, pt, n_seq, n_tokens, max_pages,
-                           c->pool_pages, cf.n_q_heads, cf.n_kv_heads, cf.head_dim};
+                           kv4_pool_pages(c), cf.n_q_heads, cf.n_kv_heads, cf.head_dim};
         const Kv4RowsPlan p = laps_kv4_rows_plan(n_seq, n_tokens, a.n_q, a.n_kv, max_pages);
         return laps_launch_kv4_rows(a, p, p.parts > 1 ? static_cast<float*>(ws) : nullptr, s);
     }
@@ -710,7 +721,7 @@ extern "C" int laps_attention_kv4(laps_ctx* c, int32_t n_seq, int32_t n_tokens, 
     return laps_launch_attention(static_cast<const bf16_t*>(q), static_cast<bf16_t*>(out), k_pool, v_pool, true, pt, max_pages, n_seq,
                                  n_tokens, reinterpret_cast<int*>(w8 + L.tile_start), reinterpret_cast<int*>(w8 + L.item_seq),
                                  reinterpret_cast<float*>(w8 + L.partial), L.total - L.partial, cf.n_q_heads, cf.n_kv_heads,
-                                 cf.head_dim, c->pool_pages, s);
+                                 cf.head_dim, kv4_pool_pages(c), s);
 }
 
 extern "C" size_t laps_gemm_workspace_bytes(int32_t m, int32_t n, int32_t k, int32_t split_k) {

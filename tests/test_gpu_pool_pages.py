@@ -1,5 +1,5 @@
-"""How many pages the pools hold (laps_ctx_set_pool_pages) is a property of each call's own pools: a captured graph keeps that of its
-capture, whatever pools of another size the same context is given afterwards."""
+"""How many pages the pools hold (laps_ctx_set_pool_pages and its 4-bit counterpart) is a property of each call's own pools: a
+captured graph keeps that of its capture, and pools of another size in the same context change nothing for it."""
 import ctypes as C
 
 import numpy as np
@@ -76,4 +76,49 @@ def test_a_graph_keeps_the_page_count_of_its_capture(between):
         for got, want in zip(pools_again, after):
             assert torch.equal(got.view(torch.int16), want.view(torch.int16))
     graph.close()
+    ctx.close()
+
+
+def raw_gather(ctx, table, kp, vp, n):
+    """laps_kv_gather of n tokens without the binding, which would say how many pages there are."""
+    cfg = ctx.cfg
+    k, v = (torch.full((n, cfg.n_kv_heads, cfg.head_dim), 3.25, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    p = lambda t: C.c_void_p(t.data_ptr())
+    cu, start, table = dev([0, n]), dev([0]), dev(table)
+    assert api.lib().laps_kv_gather(ctx._h, C.c_int32(1), C.c_int32(n), p(cu), p(start), p(table), C.c_int32(table.shape[1]), p(kp), p(vp),
+                                    p(k), p(v), None) == 0
+    torch.cuda.synchronize()
+    return k, v
+
+
+def test_4bit_calls_leave_the_bf16_count_alone():
+    cfg = inputs.tiny_cfg(1)
+    ctx = api.LapsCtx(cfg, 64)
+    kp, vp = ctx.new_pools(8, 1, zero=True)
+    table = [[6, 3, 7]]
+    assert api.lib().laps_ctx_set_pool_pages(ctx._h, C.c_int32(7)) == 0
+    write_4bit_pools(ctx, 2)
+    for got in raw_gather(ctx, table, kp[0], vp[0], 48):
+        assert bool((got[:32] == 0).all()) and bool((got[32:] == 3.25).all())      # pages 6 and 3 are inside 7 pages, 7 is not
+    write_4bit_pools(ctx, 90)
+    for got in raw_gather(ctx, table, kp[0], vp[0], 48):
+        assert bool((got[:32] == 0).all()) and bool((got[32:] == 3.25).all())
+    ctx.close()
+
+
+def test_the_4bit_count_guards_4bit_calls_and_falls_back_to_the_other():
+    """Without the binding: a token on page 5 of 8 is written where the count in force says that there is such a page."""
+    cfg = inputs.tiny_cfg(1)
+    ctx = api.LapsCtx(cfg, 64)
+    L, p = api.lib(), lambda t: t.data_ptr()
+    x = torch.ones((1, cfg.n_kv_heads, cfg.head_dim), dtype=torch.bfloat16, device="cuda")
+    cu, start, table = dev([0, 1]), dev([0]), dev([[5]])
+    for bf16_pages, kv4_pages, written in ((0, 0, True), (5, 0, False), (6, 0, True), (5, 6, True), (8, 5, False), (5, 8, True), (0, 5, False)):
+        assert L.laps_ctx_set_pool_pages(ctx._h, C.c_int32(bf16_pages)) == 0 and L.laps_ctx_set_kv4_pool_pages(ctx._h, kv4_pages) == 0
+        k4, v4 = ctx.new_kv4_pools(8, 1, zero=True)
+        assert L.laps_kv4_scatter(ctx._h, 1, 1, p(cu), p(start), p(table), 1, p(x), p(x), p(k4[0]), p(v4[0]), None) == 0
+        torch.cuda.synchronize()
+        for pool in (k4[0], v4[0]):
+            assert bool(pool[5].any()) == written and not bool(pool[:5].any()) and not bool(pool[6:].any()), (bf16_pages, kv4_pages)
+    assert L.laps_ctx_set_kv4_pool_pages(ctx._h, -1) == -1 and b"kv4_pool_pages" in L.laps_last_error()
     ctx.close()

@@ -1,0 +1,82 @@
+"""What the binding of the 4-bit calls does around the library's, on the CPU: a library that only writes down what it is asked."""
+import threading
+import time
+import types
+
+import pytest
+import torch
+
+from paper_2601_11589_amd import api, inputs
+
+CFG = inputs.tiny_cfg(1)
+
+
+class Recorder:
+    """Stands where the shared library does.  Every call that sets a page count leaves other threads time to come between."""
+
+    def __init__(self):
+        self.pages, self.used = None, {}
+
+    def __getattr__(self, name):
+        def call(handle, *args):
+            if "pool_pages" in name:
+                self.pages = getattr(args[0], "value", args[0])
+                time.sleep(0.01)
+                return 0
+            if name.endswith("_bytes"):
+                return 544
+            if name == "laps_ctx_create":
+                return 0
+            self.used.setdefault(threading.current_thread().name, []).append(self.pages)
+            return 0
+        return call
+
+
+@pytest.fixture
+def library(monkeypatch):
+    lib = Recorder()
+    monkeypatch.setattr(api, "lib", lambda: lib)
+    monkeypatch.setattr(api, "_expect", lambda what, t, dtype, shape, device: t.data_ptr())
+    monkeypatch.setattr(api, "_after_current", lambda stream: None)
+    monkeypatch.setattr(api, "_raw_stream", lambda device: 0)
+    return lib
+
+
+def arguments(n_pages):
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)
+    pool = lambda: torch.zeros((n_pages, CFG.n_kv_heads, 544), dtype=torch.uint8)
+    rows = lambda: torch.zeros((3, CFG.n_kv_heads, CFG.head_dim), dtype=torch.bfloat16)
+    q = lambda: torch.zeros((3, CFG.n_q_heads * CFG.head_dim), dtype=torch.bfloat16)
+    return types.SimpleNamespace(cu=i32(3), start=i32(2), table=i32(2, 4), lens=i32(2), k4=pool(), v4=pool(), k=rows(), v=rows(), q=q(), out=q())
+
+
+def calls(ctx, a, stream):
+    return {
+        "scatter": ([a.cu, a.start, a.table, a.k, a.v, a.k4, a.v4],
+                    lambda: ctx.laps_kv4_scatter(a.cu, a.start, a.table, a.k, a.v, a.k4, a.v4, stream=stream)),
+        "gather": ([a.cu, a.start, a.table, a.k4, a.v4, a.k, a.v],
+                   lambda: ctx.laps_kv4_gather(a.cu, a.start, a.table, a.k4, a.v4, 3, a.k, a.v, stream=stream)),
+        "attention": ([a.cu, a.lens, a.start, a.table, a.k4, a.v4, a.q, a.out],
+                      lambda: ctx.laps_attention_kv4(a.cu, a.lens, a.start, a.table, a.k4, a.v4, a.q, a.out, stream=stream)),
+    }
+
+
+@pytest.mark.parametrize("name", ["scatter", "gather", "attention"])
+def test_threads_with_pools_of_different_sizes_keep_their_counts(library, name):
+    ctx, sizes = api.LapsCtx(CFG, 64), (3, 50, 700)
+
+    def run(n_pages):
+        call = calls(ctx, arguments(n_pages), None)[name][1]
+        for _ in range(5):
+            call()
+
+    threads = [threading.Thread(target=run, args=(n,), name=str(n)) for n in sizes]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(60)
+    assert library.used == {str(n): [n] * 5 for n in sizes}
+
+
+def test_the_4bit_page_count_refuses_a_missing_context():
+    assert api.lib().laps_ctx_set_kv4_pool_pages(None, 8) == -1 and b"kv4_pool_pages" in api.lib().laps_last_error()
