@@ -129,10 +129,12 @@ def _after_current(stream):
 
 
 def _held_by(stream, *tensors):
-    """Tensors made on the current stream for work on `stream`: their memory goes to nobody else before that is done."""
-    if stream.cuda_stream != torch.cuda.current_stream().cuda_stream:
+    """Tensors that work on `stream` reads or writes, allocated as a rule on the current stream: whoever drops them now, their memory
+    goes to nobody else before that work is done.  None entries are skipped."""
+    if stream is not None and stream.cuda_stream != torch.cuda.current_stream().cuda_stream:
         for t in tensors:
-            t.record_stream(stream)
+            if t is not None:
+                t.record_stream(stream)
 
 
 def _expect(what, t, dtype, shape, device):
@@ -507,6 +509,7 @@ class LapsCtx:
         src_k, src_v = _expect("k_src", k_src, torch.bfloat16, shape, device), _expect("v_src", v_src, torch.bfloat16, shape, device)
         s = self._kv4_stream(stream, device)
         self._kv4_launch(lib().laps_kv4_scatter, k4_pool, n_seq, shape[0], cu_p, start_p, table_p, width, src_k, src_v, k_p, v_p, s)
+        _held_by(stream, cu, start_pos, page_table, k_src, v_src, k4_pool, v4_pool)
 
     def laps_kv4_gather(self, cu, start_pos, page_table, k4_pool, v4_pool, n_tokens, k_out=None, v_out=None, stream=None):
         """Reads token-major bf16 K/V back from 4-bit pools, into k_out / v_out if given.  Rows without a page keep what they
@@ -519,8 +522,7 @@ class LapsCtx:
         dst_k, dst_v = _expect("k_out", k, torch.bfloat16, shape, device), _expect("v_out", v, torch.bfloat16, shape, device)
         s = self._kv4_stream(stream, device)
         self._kv4_launch(lib().laps_kv4_gather, k4_pool, n_seq, n_tokens, cu_p, start_p, table_p, width, k_p, v_p, dst_k, dst_v, s)
-        if stream is not None:
-            _held_by(stream, *(t for t, given in ((k, k_out), (v, v_out)) if given is None))
+        _held_by(stream, cu, start_pos, page_table, k4_pool, v4_pool, k, v)
         return k, v
 
     def laps_attention_kv4_workspace_bytes(self, n_seq: int, n_tokens: int, max_pages: int) -> int:
@@ -541,8 +543,7 @@ class LapsCtx:
         s = self._kv4_stream(stream, device)
         self._kv4_launch(lib().laps_attention_kv4, k4_pool, n_seq, shape[0], cu_p, len_p, pre_p, table_p, width, k_p, v_p, q_p, y_p,
                          ws.data_ptr(), need, s)
-        if stream is not None:
-            _held_by(stream, ws, *((y,) if out is None else ()))
+        _held_by(stream, cu, seq_len, prefix_len, page_table, k4_pool, v4_pool, q, y, ws)
         return y
 
     # ---- forward

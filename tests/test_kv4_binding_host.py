@@ -62,6 +62,18 @@ def calls(ctx, a, stream):
 
 
 @pytest.mark.parametrize("name", ["scatter", "gather", "attention"])
+def test_everything_a_side_stream_reads_or_writes_is_held(library, monkeypatch, name):
+    held = []
+    monkeypatch.setattr(api, "_held_by", lambda stream, *tensors: held.extend(t for t in tensors if t is not None))
+    side = types.SimpleNamespace(cuda_stream=1)
+    given, call = calls(api.LapsCtx(CFG, 64), arguments(5), side)[name]
+    call()
+    assert all(any(h is t for h in held) for t in given), [i for i, t in enumerate(given) if not any(h is t for h in held)]
+    assert all(isinstance(t, torch.Tensor) for t in held)
+    assert name != "attention" or any(h.dtype is torch.uint8 and h.dim() == 1 for h in held)      # and the workspace
+
+
+@pytest.mark.parametrize("name", ["scatter", "gather", "attention"])
 def test_threads_with_pools_of_different_sizes_keep_their_counts(library, name):
     ctx, sizes = api.LapsCtx(CFG, 64), (3, 50, 700)
 
