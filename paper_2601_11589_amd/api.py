@@ -600,6 +600,7 @@ class LapsCtx:
         _after_current(stream)
         _check(lib().laps_gemm_bf16(self._h, _p(a), _p(w), _p(out), C.c_int32(m), C.c_int32(n), C.c_int32(k),
                                     C.c_int32(split_k), _p(ws), C.c_size_t(ws.numel()), _stream(stream)))
+        _held_by(stream, ws)
         return out
 
     def laps_gemm_plan_info(self, m, n, k, split_k=0, epilogue=0) -> dict:
@@ -620,6 +621,7 @@ class LapsCtx:
         _check(lib().laps_gemm_epilogue_bf16(self._h, _p(a), _p(w), C.c_int32(m), C.c_int32(n), C.c_int32(k),
                                              C.c_int32(epilogue), _p(resid), _p(out_f32), _p(out_bf16), _p(ws),
                                              C.c_size_t(ws.numel()), _stream(stream)))
+        _held_by(stream, ws)
         return out_f32 if epilogue == 1 else out_bf16
 
     def laps_attention(self, cu, seq_len, prefix_len, page_table, k_pool, v_pool, q, stream=None):

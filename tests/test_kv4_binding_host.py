@@ -1,4 +1,5 @@
-"""What the binding of the 4-bit calls does around the library's, on the CPU: a library that only writes down what it is asked."""
+"""What the binding does around the calls of the library (those on 4-bit pools above all), on the CPU: a library that only writes down what
+it is asked."""
 import threading
 import time
 import types
@@ -92,3 +93,13 @@ def test_threads_with_pools_of_different_sizes_keep_their_counts(library, name):
 
 def test_the_4bit_page_count_refuses_a_missing_context():
     assert api.lib().laps_ctx_set_kv4_pool_pages(None, 8) == -1 and b"kv4_pool_pages" in api.lib().laps_last_error()
+
+
+@pytest.mark.parametrize("epilogue", [0, 1, 2])
+def test_the_workspace_of_a_product_on_a_side_stream_is_held(library, monkeypatch, epilogue):
+    held = []
+    monkeypatch.setattr(api, "_held_by", lambda stream, *tensors: held.extend(tensors))
+    side, ctx = types.SimpleNamespace(cuda_stream=1), api.LapsCtx(CFG, 64)
+    a, w = torch.zeros((4, 64), dtype=torch.bfloat16), torch.zeros((64, 64), dtype=torch.bfloat16)
+    ctx.laps_gemm_epilogue_bf16(a, w, epilogue, stream=side) if epilogue else ctx.laps_gemm_bf16(a, w, 4, stream=side)
+    assert any(t.dtype is torch.uint8 for t in held)
