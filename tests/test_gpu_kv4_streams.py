@@ -64,3 +64,34 @@ def test_dropped_arguments_are_not_handed_out_again(name):
     side.synchronize()
     del busy
     ctx.close()
+
+
+def test_a_captured_step_on_a_forked_stream_with_dropped_arguments():
+    """Inside one capture: copies of the inputs, the calls on a second stream, the copies dropped, and memory of the same sizes filled on
+    the first one before the two join."""
+    ctx, side = api.LapsCtx(CFG, 64), torch.cuda.Stream()
+    a = arguments(ctx)
+    ctx.laps_kv4_scatter(a.cu, a.pre, a.table, a.k, a.v, a.k4, a.v4)
+    ctx.laps_attention_kv4(a.cu, a.lens, a.pre, a.table, a.k4, a.v4, a.q)
+    names = ("cu", "lens", "pre", "table", "k", "v", "q")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c = types.SimpleNamespace(**{n: getattr(a, n).clone() for n in names})
+        ctx.laps_kv4_scatter(c.cu, c.pre, c.table, c.k, c.v, a.k4, a.v4, stream=side)
+        out = ctx.laps_attention_kv4(c.cu, c.lens, c.pre, c.table, a.k4, a.v4, c.q, stream=side)
+        del c
+        over = [torch.full_like(getattr(a, n), 3) for n in names for _ in range(2)]
+        torch.cuda.current_stream().wait_stream(side)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    for _ in range(5):
+        for t in (a.k, a.v, a.q):
+            t.normal_(0, 1, generator=g)
+        graph.replay()
+        torch.cuda.synchronize()
+        pools = a.k4.clone(), a.v4.clone()
+        ctx.laps_kv4_scatter(a.cu, a.pre, a.table, a.k, a.v, a.k4, a.v4)
+        want = ctx.laps_attention_kv4(a.cu, a.lens, a.pre, a.table, a.k4, a.v4, a.q)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(pools[0], a.k4) and torch.equal(pools[1], a.v4)
+        assert all(bool((t == 3).all()) for t in over) and bool(want.any())
+    ctx.close()
