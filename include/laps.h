@@ -334,7 +334,9 @@ int laps_attention(laps_ctx* ctx, int32_t n_seq, int32_t n_tokens, const int32_t
  * it is K's, of the group's 32 values if it is V's.  workspace_dev: laps_attention_kv4_workspace_bytes(ctx, n_seq, n_tokens,
  * max_pages) bytes (0 on bad arguments), 256-byte aligned, for this call alone until its work is done.  EINVAL as for laps_attention, and
  * on pools, q or out that are not 16-byte aligned, more than 2^26 pages a table row, more than 2^20 sequences times query heads, or if the
- * context's device is not current; ENOMEM if the workspace is too small. */
+ * context's device is not current; ENOMEM if the workspace is too small.
+ * The launch is laid out for the mean of the sequences' new tokens: give single tokens and long turns calls of their own, one call
+ * for both takes ten times as long and more. */
 size_t laps_attention_kv4_workspace_bytes(const laps_ctx* ctx, int32_t n_seq, int32_t n_tokens, int32_t max_pages);
 int laps_attention_kv4(laps_ctx* ctx, int32_t n_seq, int32_t n_tokens, const int32_t* cu_seqlens_dev,
                        const int32_t* seq_len_dev, const int32_t* prefix_len_dev, const int32_t* page_table_dev,

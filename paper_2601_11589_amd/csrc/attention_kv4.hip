@@ -15,6 +15,9 @@
 //
 // Codes become bf16 operands exactly (one instruction a pair, the group's scale included; two permutes a pair of V's to bring keys
 // side by side).  The query rows are the G heads of a kv head for each of the sequence's new tokens, 16 a block.
+// Weights are rounded to bf16, which the second product takes, and their sum is that of the rounded ones, so that they add up to one; scores,
+// sums, O and partial results are float32.  That makes outputs 1.1 to 1.4 times as far from 64 bits as float32 weights would (1.8e-3 to
+// 2.3e-3 of the output against 1.6e-3 to 1.7e-3, most of it the output's own rounding), the same as over bf16 pools.
 // Four waves of a workgroup take every fourth pair of pages and add up in LDS.  Few sequences over long keys: a sequence's keys go out
 // in parts of equal length to workgroups of their own, and a second kernel adds those, in order.
 #include "kv4.h"
@@ -418,6 +421,8 @@ __global__ __launch_bounds__(8 * HD / 4) void attn_rows_merge_kernel(bf16_t* __r
 }
 
 // The same for at most FEW_PARTS parts: HD / 4 lanes take a (row, query head), all its parts at once, no exchange between lanes.
+// Attention with this merge / with the one above, us: 14B, 16 times 4 tokens over 4000 keys in 2 / 4 / 8 parts 23.9 / 23.3 / 29.5 and
+// 29.3 / 28.2 / 33.6; 32B, 64 tokens over 4000 in 8 parts 68.3 and 72.5, 4 turns of 32 37.3 and 46.6; 7B, one token 11.1 and 10.8.
 constexpr int FEW_PARTS = 8, FEW_THREADS = 256;
 template <int HD>
 __global__ __launch_bounds__(FEW_THREADS) void attn_rows_merge_few_kernel(bf16_t* __restrict__ out, const float* __restrict__ part_o,
@@ -497,6 +502,12 @@ int launch_rows(const Kv4Attn& a, const Kv4RowsPlan& p, float* part, hipStream_t
 // work-item table; here every 32 rows unpack them again.  This kernel / blocks, graph replays, us: 32B, 16 sequences of 4 / 16 / 64 / 96
 // tokens over 2048 keys 18 / 31 / 73 / 109 and 37 / 44 / 80 / 90 (128 to 1920 workgroups), 64 of 8 / 16 / 24 over 2000 58 / 84 / 111 and
 // 80 / 88 / 94 (1024 to 2048), of 8 / 16 over 300 22 / 30 and 21 / 24; one of 128 over 16000 70 and 100 (160).
+// Where the rule is off: it does not look at the keys, and the largest launches it takes lose over long ones (32B, 800 tokens over 4000 /
+// 16000 / 64000 keys 97 / 312 / 1180 and 100 / 282 / 1013; 7B, 1170 tokens 104 / 315 / 1175 and 108 / 288 / 1030; 32B, 16 turns of 40 over
+// 16000 323 and 262, 4 of 200 318 and 276).  Fewer than 256 workgroups of 128 rows have no blocks to go to: over bf16 pools their key ranges are
+// split.  And rows count by their mean: a long turn among single tokens is walked block after block by the few workgroups of
+// a sequence (32B, 95 tokens over 512 to 8100 keys 98 us, a turn of 350 over 4000 65, both in one call 1620, in blocks 363; 7B,
+// 127 tokens 72, a turn of 900 100, both 3008, in blocks 334).
 bool laps_kv4_takes_rows(int n_seq, int n_tokens, int n_q, int n_kv) {
     const long rows = (long)n_tokens * (n_q / n_kv), blocks = (rows + 32L * n_seq - 1) / (32L * n_seq);
     return rows <= 16L * n_seq || blocks * n_seq * n_kv <= 1024;
@@ -516,6 +527,11 @@ Kv4RowsPlan laps_kv4_rows_plan(int n_seq, int n_tokens, int n_q, int n_kv, int m
     // 64 to 10000 1 / 2 parts 86 / 67.
     // Tables of up to 8 rounds: one launch without a merge takes no longer (one token over 900 keys 9.0 us in 1 part, 9.3 in 8; 16 tokens
     // over 500 keys 7.6 and 10.7).
+    // The caps on the longest sequence's parts (rounds / 16, / 10) are coarse: 14B, 16 times 4 tokens over 4000 / 8000 / 16000 keys take 26.3 /
+    // 37.9 / 62.2 by the rule (3 / 6 / 8 parts), 23.8 / 33.1 / 54.4 in 4 parts, 23.8 / 36.1 / 61.1 in 2, 39.8 / 49.6 / 71.6 in 12; 32B, 32 tokens
+    // over 2000 / 4000 / 8000 19.2 / 29.5 / 54.7 by the rule, 15.9 / 27.0 / 50.5 in 1.  One long history among short ones keeps
+    // the parts that the batch leaves it: 32B, 95 tokens over 100 to 2000 keys and one over 100000 274 in 2 parts, 114 in 16, with
+    // which the same table without a long one takes 76 instead of 42.
     if (rounds <= 8) return {tiles, (int)blocks, 1, 1};
     const long units = blocks * n_seq * n_kv, places = tiles == 1 ? 768 : 256;
     auto within = [](long n, long most) { return n < most ? (n > 1 ? n : 1) : most; };
