@@ -8,7 +8,7 @@ Operators, each through the public binding (`paper_2601_11589_amd.api`):
 * laps_fp8_quant       bf16 rows to 8-bit floats with a scale for each block of 128 along the row
 * laps_fp8_dequant     the way back
 * laps_linear_fp8      bf16 rows times 8-bit weights: laps_fp8_quant of the rows, then
-* laps_gemm_fp8        the product of two 8-bit matrices under their scales
+* laps_gemm_fp8        the product of two 8-bit matrices under their scales, in bf16
 
 Both formats are floats of 4 exponent and 3 mantissa bits (largest 448, no infinity) under a scale 2^e, kept as the byte e + 127: e is the
 smallest integer with amax <= 448 * 2^e, cut to [-116, 119]; x / 2^e is rounded to nearest, ties to the even code, magnitudes above 448
@@ -61,8 +61,8 @@ def _case(name, kind, model, n_seq, new, pre, fresh=0.0, pad=False, spare=0, mix
                 fresh=fresh, pad=pad, spare=spare, mix=mix)
 
 
-def _matrix(name, kind, m, n, k, bf16=True):
-    return dict(name=name, kind=kind, m=m, n=n, k=k, bf16=bf16)
+def _matrix(name, kind, m, n, k):
+    return dict(name=name, kind=kind, m=m, n=n, k=k)
 
 
 def listed():
@@ -87,8 +87,8 @@ def listed():
         _matrix("linear_turns_32b", "linear", 96, 55296, 5120),
         # a chunk of a long prompt through the same: the matrix cores
         _matrix("product_chunk_32b", "product", 2048, 55296, 5120),
-        # a ragged batch of turns through the longest rows, float32 out (the residual is added to it)
-        _matrix("linear_group_7b", "linear", 573, 3584, 18944, bf16=False),
+        # a ragged batch of turns through the longest rows (down)
+        _matrix("linear_group_7b", "linear", 573, 3584, 18944),
         # one layer's gate and up weights as a checkpoint is loaded
         _matrix("round_weights_7b", "round", 37888, 0, 3584),
     ]
@@ -115,7 +115,7 @@ def draw(rng):
         if kind == "round":
             c = _matrix("", kind, min(_log(rng, 1, 40000), MOST_ROUNDED // k), 0, k)
         else:
-            c = _matrix("", kind, min(_log(rng, 1, 4096), MOST_PRODUCTS // (n * k)), n, k, bf16=rng.random() < 0.5)
+            c = _matrix("", kind, min(_log(rng, 1, 4096), MOST_PRODUCTS // (n * k)), n, k)
     elif kind == "store":
         hi = _log(rng, 1, 8192)
         n = min(_log(rng, 1, 256), max(1, MOST_STORED // hi))
@@ -210,7 +210,7 @@ def _prepare_matrix(case, seed):
     st = dict(case=case, x=x)
     if w is not None:
         st["w"], st["w_scales"] = _plain_quant(w)
-        st["out"] = torch.empty((case["m"], case["n"]), dtype=torch.bfloat16 if case["bf16"] else torch.float32, device="cuda")
+        st["out"] = torch.empty((case["m"], case["n"]), dtype=torch.bfloat16, device="cuda")
     if case["kind"] == "product":
         st["a"], st["a_scales"] = _plain_quant(x)
     return st
@@ -430,7 +430,7 @@ def work(case):
         if case["kind"] == "round":
             return {"bytes": 2 * m * (3 * k + k // BLOCK), "flops": 0}
         rows = m * k * (1 if case["kind"] == "product" else 2)
-        return {"bytes": rows + n * (k + k // BLOCK) + m * n * (2 if case["bf16"] else 4), "flops": 2 * m * n * k}
+        return {"bytes": rows + n * (k + k // BLOCK) + 2 * m * n, "flops": 2 * m * n * k}
     n_q, n_kv, hd = HEADS[case["model"]]
     new, pre, _ = (np.asarray(a, dtype=np.int64) for a in _lengths(case))
     token8 = 2 * n_kv * hd           # a token of both pools, the scales aside
