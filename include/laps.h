@@ -54,6 +54,23 @@
  *              codes [16 tokens][head_dim / 2 bytes], then scales [16 tokens][head_dim / 32]
  *     v4_pool: blocks of the same size: codes [head_dim / 8][16 tokens][4 bytes], then scales [head_dim / 32][16 tokens]
  *   two codes a byte, the lower head_dim index in the lower half.  Slots that nothing was written to may hold any bytes.
+ *
+ * 8-bit floats (laps_kv8_*, laps_attention_kv8, laps_fp8_*, laps_gemm_fp8, laps_linear_fp8): sign, 4 exponent and 3 mantissa bits, largest
+ *   448, smallest 2^-9, no infinity, 0x7f and 0xff NaN.  The values of a block share a scale 2^e, kept as the byte e + 127: e = the smallest
+ *   integer with amax <= 448 * 2^e, cut to [-116, 119], amax the largest finite magnitude of the block (0: -116).  x / 2^e is rounded to
+ *   nearest, ties to the even code, magnitudes above 448 to 448; infinities and NaN become NaN.  Reading back is exact in bf16.
+ *
+ * 8-bit K/V cache: the same pages of 16 tokens in half the bytes.  The 16 * head_dim values of a page and kv head are a block, K and V
+ *   apart.  A write that reaches a page's slot 0 begins the page anew: its scale is that of the tokens written, and the slots that it
+ *   does not write hold zeros.  A write behind slot 0 keeps the page's other slots: the scale is the larger of the old one and the one that
+ *   the new tokens need, and where it grew the others are rounded again under it (exact but for values below 2^-6 of the new scale).
+ *   A token that has an infinity or a NaN in a kv head is NaN in that whole head, and counts for no scale.
+ *     k8_pool, v8_pool: [n_pages] pages of laps_kv8_page_bytes(n_kv_heads, head_dim) bytes: a block of 16 * head_dim codes for every kv
+ *     head, then a scale byte for every kv head, padded to a multiple of 128.
+ *              K codes [16 tokens][head_dim]; V codes [head_dim / 4][4 groups of tokens][4 head_dim indices][4 tokens]
+ *
+ * 8-bit matrices: rows of laps_fp8_columns(k) = k rounded up to 128 codes, zeros behind the k-th, blocks of 128 along a row; scales
+ *   [columns / 128][laps_fp8_scale_pitch(rows) = rows rounded up to 16] bytes, block by block.
  */
 #ifndef LAPS_H
 #define LAPS_H
@@ -192,6 +209,25 @@ int laps_kv4_gather(laps_ctx* ctx, int32_t n_seq, int32_t n_tokens, const int32_
                     const int32_t* page_table_dev, int32_t max_pages, const void* k4_pool_dev, const void* v4_pool_dev,
                     void* k_dst_dev, void* v_dst_dev, void* stream);
 
+/* The same moves between token-major bf16 K/V and 8-bit pools of n_pages pages (format: above).  Page ids outside [0, n_pages) are
+ * treated as unset.  As the 4-bit moves otherwise, but that a page may be written for one sequence a call, and by one call at a
+ * time: its tokens share a scale.  EINVAL as theirs, and on n_pages < 1. */
+size_t laps_kv8_page_bytes(int32_t n_kv_heads, int32_t head_dim); /* 0 unless n_kv_heads >= 1 and head_dim is 64 or 128 */
+int laps_kv8_scatter(laps_ctx* ctx, int32_t n_seq, int32_t n_tokens, const int32_t* cu_dev, const int32_t* start_pos_dev,
+                     const int32_t* page_table_dev, int32_t max_pages, int32_t n_pages, const void* k_src_dev, const void* v_src_dev,
+                     void* k8_pool_dev, void* v8_pool_dev, void* stream);
+int laps_kv8_gather(laps_ctx* ctx, int32_t n_seq, int32_t n_tokens, const int32_t* cu_dev, const int32_t* start_pos_dev,
+                    const int32_t* page_table_dev, int32_t max_pages, int32_t n_pages, const void* k8_pool_dev, const void* v8_pool_dev,
+                    void* k_dst_dev, void* v_dst_dev, void* stream);
+
+/* bf16 rows [rows, k] <-> 8-bit matrices (format: above), for any k up to 2^22 and up to 2^24 rows.  x needs the alignment of its elements; k
+ * a multiple of 8 and x on 16 bytes are faster.  EINVAL on NULL, other shapes, codes or scales that are not 16-byte aligned, or if the
+ * context's device is not current.  laps_fp8_columns and laps_fp8_scale_pitch are 0 outside these ranges. */
+int64_t laps_fp8_columns(int64_t k);
+int64_t laps_fp8_scale_pitch(int64_t rows);
+int laps_fp8_quant(laps_ctx* ctx, const void* x_dev, int32_t rows, int32_t k, void* codes_dev, void* scales_dev, void* stream);
+int laps_fp8_dequant(laps_ctx* ctx, const void* codes_dev, const void* scales_dev, int32_t rows, int32_t k, void* x_dev, void* stream);
+
 /* ------------------------------------------------------------------ prefill forward
  * One decoder layer over a packed ragged batch (Section 2.1: L new tokens attending to H cached
  * ones; Section 3.2: the "standard prefill kernel" that un-captured batches and long chunks use).
@@ -254,7 +290,13 @@ int laps_prefill_stack_static(laps_ctx* ctx, const laps_layer_weights* w, int32_
  * parts of a sequence's keys (fewest as far as it has keys for them), workgroups of the persistent kernel (0 = a grid of blocks),
  * workspace bytes }.
  * EINVAL on NULL or unsupported shapes. */
+/* laps_attention_kv8_plan_info: the same for 8-bit pools.
+ * laps_gemm_fp8_plan_info: the product of laps_gemm_fp8.  out[5] = { tile rows, tile columns, K slices, K elements per slice,
+ * workgroups }. */
 int laps_gemm_plan_info(int32_t m, int32_t n, int32_t k, int32_t split_k, int32_t epilogue, int32_t* out);
+int laps_gemm_fp8_plan_info(int32_t m, int32_t n, int32_t k, int32_t* out);
+int laps_attention_kv8_plan_info(int32_t n_seq, int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                 int32_t max_pages, int64_t* out);
 int laps_attn_plan_info(int32_t n_seq, int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
                         int32_t max_pages, int64_t* out);
 int laps_attention_kv4_plan_info(int32_t n_seq, int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
@@ -342,6 +384,29 @@ int laps_attention_kv4(laps_ctx* ctx, int32_t n_seq, int32_t n_tokens, const int
                        const int32_t* seq_len_dev, const int32_t* prefix_len_dev, const int32_t* page_table_dev,
                        int32_t max_pages, const void* k4_pool_dev, const void* v4_pool_dev, const void* q_dev,
                        void* out_dev, void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/* The same over 8-bit pools of n_pages pages (laps_kv8_scatter); page ids outside [0, n_pages) are treated as unset.  A NaN that the cache
+ * holds reaches the rows that see its token, in the whole head, and no others.  Workspace, errors and the mean of new tokens as there. */
+size_t laps_attention_kv8_workspace_bytes(const laps_ctx* ctx, int32_t n_seq, int32_t n_tokens, int32_t max_pages);
+int laps_attention_kv8(laps_ctx* ctx, int32_t n_seq, int32_t n_tokens, const int32_t* cu_seqlens_dev, const int32_t* seq_len_dev,
+                       const int32_t* prefix_len_dev, const int32_t* page_table_dev, int32_t max_pages, int32_t n_pages,
+                       const void* k8_pool_dev, const void* v8_pool_dev, const void* q_dev, void* out_dev, void* workspace_dev,
+                       size_t workspace_bytes, void* stream);
+
+/* out[m, n] (bf16) = A[m, k] W[n, k]^T of 8-bit matrices: sums over the blocks of 2^(eA + eW) times the block's products, in float32.  The
+ * matrix instructions add the products of eight k at a time, each cut below 2^-13 of the largest of the eight: 1.5e-5 to 3e-5 of a
+ * result in the mean, where bf16 rounds at 2^-9.  Any m, n and k; out needs the alignment of its elements.  A NaN code makes the rows or
+ * columns NaN that it belongs to.  workspace_dev: laps_gemm_fp8_workspace_bytes(m, n, k) bytes, 256-byte aligned, for this call alone until
+ * its work is done; NULL if that is 0.  EINVAL on NULL, unsupported shapes (as laps_fp8_quant; more than 2^24 tiles of 256 x 256), codes or scales
+ * that are not 16-byte aligned, or if the context's device is not current; ENOMEM if the workspace is too small. */
+size_t laps_gemm_fp8_workspace_bytes(int32_t m, int32_t n, int32_t k);
+int laps_gemm_fp8(laps_ctx* ctx, const void* a_dev, const void* a_scales_dev, const void* w_dev, const void* w_scales_dev, void* out_dev,
+                  int32_t m, int32_t n, int32_t k, void* workspace_dev, size_t workspace_bytes, void* stream);
+/* A projection of bf16 rows: laps_fp8_quant of x [m, k] into the workspace (laps_linear_fp8_workspace_bytes(m, n, k) bytes, 256-byte
+ * aligned), then laps_gemm_fp8. */
+size_t laps_linear_fp8_workspace_bytes(int32_t m, int32_t n, int32_t k);
+int laps_linear_fp8(laps_ctx* ctx, const void* x_dev, const void* w_dev, const void* w_scales_dev, void* out_dev, int32_t m, int32_t n,
+                    int32_t k, void* workspace_dev, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------ per-kernel timing
  * When enabled, un-captured laps_prefill_* calls bracket every kernel launch with HIP events on

@@ -93,6 +93,18 @@ def lib():
         L.laps_kv4_scatter.argtypes = L.laps_kv4_gather.argtypes = [p, i, i, p, p, p, i, p, p, p, p, p]
         L.laps_attention_kv4_workspace_bytes.argtypes = [p, i, i, i]
         L.laps_attention_kv4.argtypes = [p, i, i, p, p, p, p, i, p, p, p, p, p, C.c_size_t, p]
+        z, w = C.c_size_t, C.c_int64
+        L.laps_kv8_page_bytes.argtypes, L.laps_kv8_page_bytes.restype = [i, i], z
+        L.laps_kv8_scatter.argtypes = L.laps_kv8_gather.argtypes = [p, i, i, p, p, p, i, i, p, p, p, p, p]
+        L.laps_attention_kv8_workspace_bytes.argtypes, L.laps_attention_kv8_workspace_bytes.restype = [p, i, i, i], z
+        L.laps_attention_kv8.argtypes = [p, i, i, p, p, p, p, i, i, p, p, p, p, p, z, p]
+        L.laps_fp8_columns.argtypes = L.laps_fp8_scale_pitch.argtypes = [w]
+        L.laps_fp8_columns.restype = L.laps_fp8_scale_pitch.restype = w
+        L.laps_fp8_quant.argtypes, L.laps_fp8_dequant.argtypes = [p, p, i, i, p, p, p], [p, p, p, i, i, p, p]
+        L.laps_gemm_fp8_workspace_bytes.argtypes = L.laps_linear_fp8_workspace_bytes.argtypes = [i, i, i]
+        L.laps_gemm_fp8_workspace_bytes.restype = L.laps_linear_fp8_workspace_bytes.restype = z
+        L.laps_gemm_fp8.argtypes = [p, p, p, p, p, p, i, i, i, p, z, p]
+        L.laps_linear_fp8.argtypes = [p, p, p, p, p, i, i, i, p, z, p]
         _lib = L
     return _lib
 
@@ -140,7 +152,7 @@ def _held_by(stream, *tensors):
 def _expect(what, t, dtype, shape, device):
     """Refuses a tensor that a kernel would read past or misread; returns its address."""
     if t.dtype is not dtype or t.shape != shape or t.get_device() != device or device < 0 or not t.is_contiguous():
-        raise LapsError(f"{what}: need a contiguous {dtype} tensor of shape {list(shape)} on the GPU of k4_pool, "
+        raise LapsError(f"{what}: need a contiguous {dtype} tensor of shape {list(shape)} on the GPU of the pools or weights, "
                         f"got {t.dtype} {list(t.shape)} on {t.device}")
     return t.data_ptr()
 
@@ -388,6 +400,7 @@ class LapsCtx:
         self._ws = None
         self._kv4_block = lib().laps_kv4_block_bytes(cfg.head_dim)
         self._kv4_lock = threading.Lock()
+        self._kv8_page = lib().laps_kv8_page_bytes(cfg.n_kv_heads, cfg.head_dim)
 
     def close(self):
         if self._h:
@@ -488,7 +501,7 @@ class LapsCtx:
                 _expect("page_table", page_table, torch.int32, (n_seq, width), device),
                 _expect("k4_pool", k4_pool, torch.uint8, pools, device), _expect("v4_pool", v4_pool, torch.uint8, pools, device))
 
-    def _kv4_stream(self, stream, device):
+    def _launch_stream(self, stream, device):
         if stream is None:   # the address alone where torch hands it out: 1 us less than with a stream object around it
             return _raw_stream(device) if _raw_stream else torch.cuda.current_stream(device).cuda_stream
         _after_current(stream)
@@ -507,7 +520,7 @@ class LapsCtx:
         shape = (k_src.shape[0], self.cfg.n_kv_heads, self.cfg.head_dim)
         start_p = _expect("start_pos", start_pos, torch.int32, (n_seq,), device)
         src_k, src_v = _expect("k_src", k_src, torch.bfloat16, shape, device), _expect("v_src", v_src, torch.bfloat16, shape, device)
-        s = self._kv4_stream(stream, device)
+        s = self._launch_stream(stream, device)
         self._kv4_launch(lib().laps_kv4_scatter, k4_pool, n_seq, shape[0], cu_p, start_p, table_p, width, src_k, src_v, k_p, v_p, s)
         _held_by(stream, cu, start_pos, page_table, k_src, v_src, k4_pool, v4_pool)
 
@@ -520,7 +533,7 @@ class LapsCtx:
         k = torch.empty(shape, dtype=torch.bfloat16, device=k4_pool.device) if k_out is None else k_out
         v = torch.empty(shape, dtype=torch.bfloat16, device=k4_pool.device) if v_out is None else v_out
         dst_k, dst_v = _expect("k_out", k, torch.bfloat16, shape, device), _expect("v_out", v, torch.bfloat16, shape, device)
-        s = self._kv4_stream(stream, device)
+        s = self._launch_stream(stream, device)
         self._kv4_launch(lib().laps_kv4_gather, k4_pool, n_seq, n_tokens, cu_p, start_p, table_p, width, k_p, v_p, dst_k, dst_v, s)
         _held_by(stream, cu, start_pos, page_table, k4_pool, v4_pool, k, v)
         return k, v
@@ -540,10 +553,132 @@ class LapsCtx:
         y_p = _expect("out", y, torch.bfloat16, shape, device)
         need = lib().laps_attention_kv4_workspace_bytes(self._h, n_seq, shape[0], width)
         ws = torch.empty(need or 256, dtype=torch.uint8, device=q.device)
-        s = self._kv4_stream(stream, device)
+        s = self._launch_stream(stream, device)
         self._kv4_launch(lib().laps_attention_kv4, k4_pool, n_seq, shape[0], cu_p, len_p, pre_p, table_p, width, k_p, v_p, q_p, y_p,
                          ws.data_ptr(), need, s)
         _held_by(stream, cu, seq_len, prefix_len, page_table, k4_pool, v4_pool, q, y, ws)
+        return y
+
+    # ---- 8-bit KV pools
+    def new_kv8_pools(self, n_pages: int, n_layers: int | None = None, zero: bool = False):
+        mk = torch.zeros if zero else torch.empty
+        k8, v8 = ([mk((n_pages, self._kv8_page), dtype=torch.uint8, device="cuda") for _ in range(n_layers or self.cfg.n_layers)] for _ in range(2))
+        return k8, v8
+
+    def _kv8_call(self, cu, page_table, k8_pool, v8_pool):
+        """As _kv4_call, and the pools' pages."""
+        n_seq, width, device = cu.numel() - 1, page_table.shape[-1], k8_pool.get_device()
+        n_pages = k8_pool.shape[0]
+        pools = (n_pages, self._kv8_page)
+        return (n_seq, width, n_pages, device, _expect("cu", cu, torch.int32, (n_seq + 1,), device),
+                _expect("page_table", page_table, torch.int32, (n_seq, width), device),
+                _expect("k8_pool", k8_pool, torch.uint8, pools, device), _expect("v8_pool", v8_pool, torch.uint8, pools, device))
+
+    def laps_kv8_scatter(self, cu, start_pos, page_table, k_src, v_src, k8_pool, v8_pool, stream=None):
+        """Quantises token-major bf16 K/V [n_tokens, n_kv_heads, head_dim] into 8-bit pools (new_kv8_pools)."""
+        n_seq, width, n_pages, device, cu_p, table_p, k_p, v_p = self._kv8_call(cu, page_table, k8_pool, v8_pool)
+        shape = (k_src.shape[0], self.cfg.n_kv_heads, self.cfg.head_dim)
+        start_p = _expect("start_pos", start_pos, torch.int32, (n_seq,), device)
+        src_k, src_v = _expect("k_src", k_src, torch.bfloat16, shape, device), _expect("v_src", v_src, torch.bfloat16, shape, device)
+        s = self._launch_stream(stream, device)
+        _check(lib().laps_kv8_scatter(self._h, n_seq, shape[0], cu_p, start_p, table_p, width, n_pages, src_k, src_v, k_p, v_p, s))
+        _held_by(stream, cu, start_pos, page_table, k_src, v_src, k8_pool, v8_pool)
+
+    def laps_kv8_gather(self, cu, start_pos, page_table, k8_pool, v8_pool, n_tokens, k_out=None, v_out=None, stream=None):
+        """Reads token-major bf16 K/V back from 8-bit pools, into k_out / v_out if given.  Rows without a page keep what they
+        held (nothing defined in tensors made here)."""
+        n_seq, width, n_pages, device, cu_p, table_p, k_p, v_p = self._kv8_call(cu, page_table, k8_pool, v8_pool)
+        shape = (n_tokens, self.cfg.n_kv_heads, self.cfg.head_dim)
+        start_p = _expect("start_pos", start_pos, torch.int32, (n_seq,), device)
+        k = torch.empty(shape, dtype=torch.bfloat16, device=k8_pool.device) if k_out is None else k_out
+        v = torch.empty(shape, dtype=torch.bfloat16, device=k8_pool.device) if v_out is None else v_out
+        dst_k, dst_v = _expect("k_out", k, torch.bfloat16, shape, device), _expect("v_out", v, torch.bfloat16, shape, device)
+        s = self._launch_stream(stream, device)
+        _check(lib().laps_kv8_gather(self._h, n_seq, n_tokens, cu_p, start_p, table_p, width, n_pages, k_p, v_p, dst_k, dst_v, s))
+        _held_by(stream, cu, start_pos, page_table, k8_pool, v8_pool, k, v)
+        return k, v
+
+    def laps_attention_kv8_workspace_bytes(self, n_seq: int, n_tokens: int, max_pages: int) -> int:
+        return lib().laps_attention_kv8_workspace_bytes(self._h, n_seq, n_tokens, max_pages)
+
+    def laps_attention_kv8(self, cu, seq_len, prefix_len, page_table, k8_pool, v8_pool, q, out=None, stream=None):
+        """laps_attention over 8-bit pools.  Rows of `out` that hold no token keep what they held (zeros if made here).  The
+        workspace is this call's own."""
+        n_seq, width, n_pages, device, cu_p, table_p, k_p, v_p = self._kv8_call(cu, page_table, k8_pool, v8_pool)
+        shape = (q.shape[0], self.cfg.n_q_heads * self.cfg.head_dim)
+        len_p = None if seq_len is None else _expect("seq_len", seq_len, torch.int32, (n_seq,), device)
+        pre_p = _expect("prefix_len", prefix_len, torch.int32, (n_seq,), device)
+        q_p = _expect("q", q, torch.bfloat16, shape, device)
+        y = torch.zeros_like(q) if out is None else out
+        y_p = _expect("out", y, torch.bfloat16, shape, device)
+        need = lib().laps_attention_kv8_workspace_bytes(self._h, n_seq, shape[0], width)
+        ws = torch.empty(need or 256, dtype=torch.uint8, device=q.device)
+        s = self._launch_stream(stream, device)
+        _check(lib().laps_attention_kv8(self._h, n_seq, shape[0], cu_p, len_p, pre_p, table_p, width, n_pages, k_p, v_p, q_p, y_p,
+                                        ws.data_ptr(), need, s))
+        _held_by(stream, cu, seq_len, prefix_len, page_table, k8_pool, v8_pool, q, y, ws)
+        return y
+
+    # ---- 8-bit matrices
+    def _fp8_matrix(self, what, codes, scales, k, device):
+        """Checks codes [rows, k rounded up to 128] and their scales: returns rows and addresses."""
+        rows, columns = codes.shape[0], lib().laps_fp8_columns(k)
+        return (rows, _expect(what, codes, torch.uint8, (rows, columns), device),
+                _expect(what + " scales", scales, torch.uint8, (columns // 128, lib().laps_fp8_scale_pitch(rows)), device))
+
+    def laps_fp8_quant(self, x, codes=None, scales=None, stream=None):
+        """bf16 [rows, k] -> 8-bit floats (uint8 [rows, k rounded up to 128], zeros behind k; views as torch.float8_e4m3fn) and their scale
+        bytes (uint8 [blocks of 128, rows rounded up to 16])."""
+        (rows, k), device = x.shape, x.get_device()
+        columns = lib().laps_fp8_columns(k)
+        x_p = _expect("x", x, torch.bfloat16, (rows, k), device)
+        codes = torch.empty((rows, columns), dtype=torch.uint8, device=x.device) if codes is None else codes
+        scales = torch.empty((columns // 128, lib().laps_fp8_scale_pitch(rows)), dtype=torch.uint8, device=x.device) if scales is None else scales
+        _, codes_p, scales_p = self._fp8_matrix("codes", codes, scales, k, device)
+        if codes.shape[0] != rows:
+            raise LapsError(f"codes: need {rows} rows, got {codes.shape[0]}")
+        s = self._launch_stream(stream, device)
+        _check(lib().laps_fp8_quant(self._h, x_p, rows, k, codes_p, scales_p, s))
+        _held_by(stream, x, codes, scales)
+        return codes, scales
+
+    def laps_fp8_dequant(self, codes, scales, k, out=None, stream=None):
+        """The way back: bf16 [rows, k], exactly what the codes stand for."""
+        device = codes.get_device()
+        rows, codes_p, scales_p = self._fp8_matrix("codes", codes, scales, k, device)
+        y = torch.empty((rows, k), dtype=torch.bfloat16, device=codes.device) if out is None else out
+        y_p = _expect("out", y, torch.bfloat16, (rows, k), device)
+        s = self._launch_stream(stream, device)
+        _check(lib().laps_fp8_dequant(self._h, codes_p, scales_p, rows, k, y_p, s))
+        _held_by(stream, codes, scales, y)
+        return y
+
+    def laps_gemm_fp8(self, a, a_scales, w, w_scales, out=None, stream=None):
+        """bf16 [m, n] = a w^T of 8-bit matrices (laps_fp8_quant) of equal width.  The workspace is this call's own."""
+        device, k = w.get_device(), w.shape[1]
+        m, a_p, as_p = self._fp8_matrix("a", a, a_scales, k, device)
+        n, w_p, ws_p = self._fp8_matrix("w", w, w_scales, k, device)
+        y = torch.empty((m, n), dtype=torch.bfloat16, device=w.device) if out is None else out
+        y_p = _expect("out", y, torch.bfloat16, (m, n), device)
+        need = lib().laps_gemm_fp8_workspace_bytes(m, n, k)
+        ws = torch.empty(need, dtype=torch.uint8, device=w.device) if need else None
+        s = self._launch_stream(stream, device)
+        _check(lib().laps_gemm_fp8(self._h, a_p, as_p, w_p, ws_p, y_p, m, n, k, ws.data_ptr() if need else None, need, s))
+        _held_by(stream, a, a_scales, w, w_scales, y, ws)
+        return y
+
+    def laps_linear_fp8(self, x, w, w_scales, out=None, stream=None):
+        """bf16 [m, n] = x w^T: laps_fp8_quant of the bf16 rows x [m, k], then laps_gemm_fp8."""
+        (m, k), device = x.shape, w.get_device()
+        x_p = _expect("x", x, torch.bfloat16, (m, k), device)
+        n, w_p, ws_p = self._fp8_matrix("w", w, w_scales, k, device)
+        y = torch.empty((m, n), dtype=torch.bfloat16, device=w.device) if out is None else out
+        y_p = _expect("out", y, torch.bfloat16, (m, n), device)
+        need = lib().laps_linear_fp8_workspace_bytes(m, n, k)
+        ws = torch.empty(need or 256, dtype=torch.uint8, device=w.device)
+        s = self._launch_stream(stream, device)
+        _check(lib().laps_linear_fp8(self._h, x_p, w_p, ws_p, y_p, m, n, k, ws.data_ptr(), need, s))
+        _held_by(stream, x, w, w_scales, y, ws)
         return y
 
     # ---- forward

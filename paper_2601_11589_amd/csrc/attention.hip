@@ -35,6 +35,7 @@
 // blocks of very different lengths.  Such launches run the 8-wave loop in a fixed number of workgroups, each of which walks
 // an equal share of the batch's (kv head, row block) units, worked out on the device from the batch's lengths; a unit cut
 // between shares leaves partial results like a split key range, merged in key order by a kernel of its own.
+#include "fp8.h"
 #include "kv4.h"
 #include "laps_internal.h"
 
@@ -57,8 +58,9 @@ constexpr int MIN_TILES_PER_SPLIT = 4;   // key tiles per part of a split key ra
 // HALVES: the 4-wave loop forms its probabilities and row sums by half tiles, as the 8-wave loop does: the same bits.
 // PERSIST: a fixed number of workgroups, each walking its share of the batch (laps_dev_attn_bounds); a share may begin
 // and end inside a unit, whose parts then go through partial results like the splits.
-// KV4: 4-bit pools (kv4.h).  Their codes travel as they are and become bf16 (exactly) on the way into LDS; all else is the same.
-template <int HD, int NW, bool SPLIT, bool PERSIST, bool HALVES = false, bool KV4 = false>
+// BITS: 16 = bf16 pools, 4 and 8 = quantised ones (kv4.h, fp8.h).  Their codes travel as they are and become bf16 (exactly) on the way into
+// LDS; all else is the same.
+template <int HD, int NW, bool SPLIT, bool PERSIST, bool HALVES = false, int BITS = 16>
 __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const bf16_t* __restrict__ q, bf16_t* __restrict__ out,
                                                         float* __restrict__ part_o, float* __restrict__ part_ml,
                                                         const bf16_t* __restrict__ k_pool,
@@ -68,7 +70,8 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const bf16_t* __restri
                                                         const int* __restrict__ tile_start, int n_seq, int n_q,
                                                         int n_kv, float scale_log2e, int n_pool_pages, int n_tokens,
                                                         int max_items, const int4* __restrict__ bounds) {
-    static_assert(!SPLIT || !KV4, "key ranges of 4-bit pools are split in the kernel for few rows");
+    constexpr bool KV4 = BITS == 4, KV8 = BITS == 8, QUANT = KV4 || KV8;
+    static_assert(!SPLIT || !QUANT, "key ranges of quantised pools are split in the kernel for few rows");
     constexpr int NTHR = NW * 64;
     constexpr int CPR = HD / 8;            // 16-byte chunks per K row
     constexpr int CPP = HD * 2;            // 16-byte chunks per page (K and V alike)
@@ -80,7 +83,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const bf16_t* __restri
 
     __shared__ __align__(16) u32x4 Ks[2][KT * CPR];   // double buffered: one barrier per tile
     __shared__ __align__(16) u32x4 Vs[2][HD * 8];
-    __shared__ int nan_first[KV4 ? NI : 1];   // first key whose V group is NaN, among those that not every row of the unit sees
+    __shared__ int nan_first[KV4 ? NI : 1];   // first key whose V (4 bits: group of V) is NaN, among those that not every row of the unit sees
 
     const int G = n_q / n_kv;
     // one unit: (item, kv head), key tiles [t0, t1) of it if PERSIST; slot: where a cut unit's result goes
@@ -144,14 +147,16 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const bf16_t* __restri
     u32x4 kreg[NLD], vreg[NLD];   // landing registers of the tile copy
     // KV4: a piece is 16 bytes of codes, 32 head_dim indices of a key or 8 of four keys, with its scales.  A tile has PIECES of K
     // and of V; where there are threads for both, the upper half of them takes V's.
-    constexpr int PIECES = KT * HD / 32, PPP = HD / 2;   // in a tile, in a page
-    constexpr bool BOTH = PIECES == NTHR;
-    constexpr int NID = KV4 ? 1 : NLD;                   // page ids a thread needs for its share of a tile
+    // KV8: a piece is 16 bytes of codes, 16 head_dim indices of a key or 4 of four keys; a wave's pieces lie in one page.
+    constexpr int PIECES = KT * HD / (KV8 ? 16 : 32), PPP = KV8 ? HD : HD / 2;   // in a tile, in a page
+    constexpr bool BOTH = KV8 ? NTHR == 256 : PIECES == NTHR;
+    constexpr int NP = KV8 ? PIECES / 256 : 1;           // pieces of K or V a thread takes, a quarter or half of a tile apart
+    constexpr int NID = QUANT ? NP : NLD;                // page ids a thread needs for its share of a tile
     const int piece = BOTH ? tid : tid % (NTHR / 2), in_page = piece % PPP;
     const bool has_piece = piece < PIECES, takes_k = has_piece && (BOTH || tid < NTHR / 2), takes_v = has_piece && (BOTH || tid >= NTHR / 2);
-    [[maybe_unused]] unsigned kscale = 0, vscale = 0;
+    [[maybe_unused]] unsigned kscale[NP], vscale[NP];
     auto page_id = [&](int j0, int i) -> int {
-        const int in_tile = KV4 ? piece / PPP : (tid + i * NTHR) / CPP;
+        const int in_tile = QUANT ? (piece + i * 256) / PPP : (tid + i * NTHR) / CPP;
         int pidx = j0 / LAPS_PAGE + (KV4 && HD == 64 ? in_tile : __builtin_amdgcn_readfirstlane(in_tile));
         pidx = pidx < n_pages_seq ? pidx : n_pages_seq - 1;  // past the end: any valid page, masked later
         return pt[pidx];
@@ -168,7 +173,16 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const bf16_t* __restri
             const size_t page = (size_t)((id[0] > 0 && id[0] < n_pool_pages) ? id[0] : 0);
             const unsigned char* block = reinterpret_cast<const unsigned char*>(k_pool) + (page * n_kv + kvh) * kv4_block(HD);
             kreg[0] = reinterpret_cast<const u32x4*>(block)[in_page];
-            kscale = block[kv4_codes(HD) + in_page];
+            kscale[0] = block[kv4_codes(HD) + in_page];
+        } else if constexpr (KV8) {
+            if (!takes_k) return;
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                const size_t page = (size_t)((id[i] > 0 && id[i] < n_pool_pages) ? id[i] : 0);
+                const unsigned char* held = reinterpret_cast<const unsigned char*>(k_pool) + page * kv8_page(n_kv, HD);
+                kreg[i] = reinterpret_cast<const u32x4*>(held)[kvh * PPP + in_page];
+                kscale[i] = held[n_kv * kv8_codes(HD) + kvh];
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < NLD; ++i) kreg[i] = reinterpret_cast<const u32x4*>(k_pool)[chunk_offset(id[i], i)];
@@ -180,7 +194,16 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const bf16_t* __restri
             const size_t page = (size_t)((id[0] > 0 && id[0] < n_pool_pages) ? id[0] : 0);
             const unsigned char* block = reinterpret_cast<const unsigned char*>(v_pool) + (page * n_kv + kvh) * kv4_block(HD);
             vreg[0] = reinterpret_cast<const u32x4*>(block)[in_page];
-            vscale = reinterpret_cast<const unsigned*>(block + kv4_codes(HD))[in_page / 16 * 4 + in_page % 4];
+            vscale[0] = reinterpret_cast<const unsigned*>(block + kv4_codes(HD))[in_page / 16 * 4 + in_page % 4];
+        } else if constexpr (KV8) {
+            if (!takes_v) return;
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                const size_t page = (size_t)((id[i] > 0 && id[i] < n_pool_pages) ? id[i] : 0);
+                const unsigned char* held = reinterpret_cast<const unsigned char*>(v_pool) + page * kv8_page(n_kv, HD);
+                vreg[i] = reinterpret_cast<const u32x4*>(held)[kvh * PPP + in_page];
+                vscale[i] = held[n_kv * kv8_codes(HD) + kvh];
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < NLD; ++i) vreg[i] = reinterpret_cast<const u32x4*>(v_pool)[chunk_offset(id[i], i)];
@@ -190,11 +213,25 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const bf16_t* __restri
         if constexpr (KV4) {
             if (!takes_k) return;
             const int key = piece / (HD / 32), g = piece % (HD / 32);
-            const float sc = kv4_scale<0>(kscale);
+            const float sc = kv4_scale<0>(kscale[0]);
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 const int kc = 4 * g + c;
                 Ks[buf][key * CPR + (CPR == 16 ? swz16(key, kc) : swz8(key, kc))] = kv4_eight(kreg[0][c], sc);
+            }
+            return;
+        }
+        if constexpr (KV8) {
+            if (!takes_k) return;
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                const int at = piece + i * 256, key = at / (HD / 16), c16 = at % (HD / 16);
+                const float sc = fp8_scale(kscale[i]);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int kc = 2 * c16 + h;
+                    Ks[buf][key * CPR + (CPR == 16 ? swz16(key, kc) : swz8(key, kc))] = fp8_eight(kreg[i][2 * h], kreg[i][2 * h + 1], sc);
+                }
             }
             return;
         }
@@ -211,7 +248,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const bf16_t* __restri
             if (!takes_v) return;
             const int c8 = in_page / 4, key = piece / PPP * LAPS_PAGE + in_page % 4 * 4;
             u32x4 v = vreg[0];
-            unsigned sc = vscale;
+            unsigned sc = vscale[0];
             if (j0 + KT - 1 > H + R0 / G) {   // some row of the unit does not see all of the tile's keys
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -239,6 +276,34 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const bf16_t* __restri
             row_pair(std::integral_constant<int, 1>{});
             row_pair(std::integral_constant<int, 2>{});
             row_pair(std::integral_constant<int, 3>{});
+            return;
+        }
+        if constexpr (KV8) {   // [HD / 4][4 groups of keys][4][4 keys]: four keys of four head_dim indices
+            if (!takes_v) return;
+            const bool ragged = j0 + KT - 1 > H + R0 / G;   // some row of the unit does not see all of the tile's keys
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                const int key = (piece + i * 256) / PPP * LAPS_PAGE + in_page % 4 * 4;
+                u32x4 v = vreg[i];
+                if (ragged) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int k = j0 + key + e;
+                        const bool past = k >= kv_len, is_nan = (v.x >> (8 * e) & 127u) == 127u;   // a token's head as a whole
+                        if (past || is_nan) {   // as above
+                            if (!past) atomicMin(&nan_first[0], k);
+                            v &= ~(255u << (8 * e));
+                        }
+                    }
+                }
+                const float sc = fp8_scale(vscale[i]);
+                u32x2* dst = reinterpret_cast<u32x2*>(Vs[buf]);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int row = in_page / 4 * 4 + w;
+                    dst[(row * 8 + swz8(row, key / 8)) * 2 + (key / 4 & 1)] = fp8_four(v[w], sc);
+                }
+            }
             return;
         }
         const bool tail = (j0 + KT > kv_len);
@@ -418,9 +483,9 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const bf16_t* __restri
     };
 
     const auto exists = [&](int j) { return j < kv_end; };
-    if constexpr (KV4) {   // before the first store of V, after the last look of the unit before
+    if constexpr (QUANT) {   // before the first store of V, after the last look of the unit before
         if (PERSIST) __syncthreads();
-        if (tid < NI) nan_first[tid] = INT_MAX;
+        if (tid < (KV4 ? NI : 1)) nan_first[tid] = INT_MAX;
         __syncthreads();
     }
     if constexpr (NW == 8) {
@@ -573,7 +638,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const bf16_t* __restri
             for (int i = 0; i < NID; ++i) pgn[i] = page_id(j0, i);
         };
         auto load_tile = [&]() {   // uses the ids load_pages fetched
-            if constexpr (KV4) {
+            if constexpr (QUANT) {
                 load_k_of(pgn);
                 load_v_of(pgn);
                 return;
@@ -630,11 +695,11 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kernel(const bf16_t* __restri
         }
     }
 
-    if constexpr (KV4) {
+    if constexpr (QUANT) {
         __syncthreads();   // V of the last tile is stored
 #pragma unroll
         for (int ni = 0; ni < NI; ++ni)
-            if (nan_first[ni] <= limit) {
+            if (nan_first[KV4 ? ni : 0] <= limit) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[ni][i] = __builtin_nanf("");
             }
@@ -836,26 +901,26 @@ __global__ __launch_bounds__(128 * MERGE_GROUPS) void attn_merge_kernel(
     }
 }
 
-template <int HD, int NW, bool HALVES, bool KV4>
+template <int HD, int NW, bool HALVES, int BITS>
 int launch_attn(const bf16_t* q, bf16_t* out, const bf16_t* k_pool, const bf16_t* v_pool, const int4* desc,
                 const int* page_table, int max_pages, const int* tile_start, int n_seq, int max_items, int n_q, int n_kv, int n_pool_pages, int n_tokens,
                 hipStream_t s) {
     const float scale_log2e = 1.4426950408889634f / sqrtf((float)HD);
-    hipLaunchKernelGGL((attn_kernel<HD, NW, false, false, HALVES, KV4>), dim3(max_items, n_kv), dim3(NW * 64), 0, s, q, out, nullptr,
+    hipLaunchKernelGGL((attn_kernel<HD, NW, false, false, HALVES, BITS>), dim3(max_items, n_kv), dim3(NW * 64), 0, s, q, out, nullptr,
                        nullptr, k_pool, v_pool, desc, page_table, max_pages, tile_start,
                        n_seq, n_q, n_kv, scale_log2e, n_pool_pages, n_tokens, max_items, nullptr);
     LAPS_LAUNCH_CHECK();
     return LAPS_OK;
 }
 
-template <int HD, bool KV4>
+template <int HD, int BITS>
 int launch_attn_persistent(const bf16_t* q, bf16_t* out, float* part, int n_wgs, const int4* bounds, const bf16_t* k_pool,
                            const bf16_t* v_pool, const int4* desc,
                            const int* page_table, int max_pages, const int* tile_start, int n_seq,
                            int max_items, int n_q, int n_kv, int n_pool_pages, int n_tokens, hipStream_t s) {
     const float scale_log2e = 1.4426950408889634f / sqrtf((float)HD);
     float* part_ml = part + (size_t)2 * n_wgs * LAPS_ATTN_LONG_ROWS * HD;
-    hipLaunchKernelGGL((attn_kernel<HD, 8, false, true, false, KV4>), dim3(n_wgs), dim3(512), 0, s, q, out, part, part_ml, k_pool, v_pool,
+    hipLaunchKernelGGL((attn_kernel<HD, 8, false, true, false, BITS>), dim3(n_wgs), dim3(512), 0, s, q, out, part, part_ml, k_pool, v_pool,
                        desc, page_table, max_pages, tile_start, n_seq, n_q, n_kv,
                        scale_log2e, n_pool_pages, n_tokens, max_items, bounds);
     LAPS_LAUNCH_CHECK();
@@ -1015,7 +1080,7 @@ int laps_attn_persistent_wgs(int n_seq, int n_tokens, int group, int n_kv, int h
     return wgs;
 }
 
-template <int HD, bool KV4>
+template <int HD, int BITS>
 static int launch_attention(const bf16_t* q, bf16_t* out, const bf16_t* k_pool, const bf16_t* v_pool, const int* page_table, int max_pages,
                             int n_seq, int n_tokens, const int* tile_start, const int* item_seq, float* partial, size_t partial_bytes,
                             int n_q, int n_kv, int n_pool_pages, hipStream_t s) {
@@ -1026,10 +1091,10 @@ static int launch_attention(const bf16_t* q, bf16_t* out, const bf16_t* k_pool, 
     int4 *bounds, *desc;
     laps_attn_item_tables(const_cast<int*>(item_seq), n_tokens, n_seq, n_q / n_kv, &pre, &bounds, &desc);
     if (n_wgs > 0)
-        return launch_attn_persistent<HD, KV4>(q, out, partial, n_wgs, bounds, k_pool, v_pool, desc, page_table, max_pages, tile_start,
+        return launch_attn_persistent<HD, BITS>(q, out, partial, n_wgs, bounds, k_pool, v_pool, desc, page_table, max_pages, tile_start,
                                                n_seq, max_items, n_q, n_kv, n_pool_pages, n_tokens, s);
     if (n_split > 1) {
-        if (!partial || KV4) {   // launches this small over 4-bit pools have a kernel of their own
+        if (!partial || BITS != 16) {   // launches this small over quantised pools have a kernel of their own
             laps_set_error("attention: key-split launch needs the partial-result workspace and bf16 pools");
             return LAPS_EINVAL;
         }
@@ -1040,20 +1105,34 @@ static int launch_attention(const bf16_t* q, bf16_t* out, const bf16_t* k_pool, 
     // does not show in the result (the sums of rounded probabilities are also the ones that match the second product:
     // 32B prompts of 64 tokens 1.79e-3 from 64 bits, with sums of unrounded ones 1.81e-3; the same time)
     const bool halves = (long)n_tokens * (n_q / n_kv) > 128L * n_seq;
-    auto launch = mt == 2 ? launch_attn<HD, 8, false, KV4> : halves ? launch_attn<HD, 4, true, KV4> : launch_attn<HD, 4, false, KV4>;
+    auto launch = mt == 2 ? launch_attn<HD, 8, false, BITS> : halves ? launch_attn<HD, 4, true, BITS> : launch_attn<HD, 4, false, BITS>;
     return launch(q, out, k_pool, v_pool, desc, page_table, max_pages, tile_start, n_seq, max_items, n_q, n_kv, n_pool_pages, n_tokens, s);
+}
+
+static int launch_by_bits(int bits, const bf16_t* q, bf16_t* out, const void* k_pool, const void* v_pool, const int* page_table, int max_pages,
+                          int n_seq, int n_tokens, const int* tile_start, const int* item_seq, float* partial, size_t partial_bytes, int n_q,
+                          int n_kv, int hd, int n_pool_pages, hipStream_t s) {
+    if (hd != 64 && hd != 128) {
+        laps_set_error("attention: head_dim %d not supported (64 or 128)", hd);
+        return LAPS_EINVAL;
+    }
+    auto launch = hd == 128 ? (bits == 4 ? launch_attention<128, 4> : bits == 8 ? launch_attention<128, 8> : launch_attention<128, 16>)
+                            : (bits == 4 ? launch_attention<64, 4> : bits == 8 ? launch_attention<64, 8> : launch_attention<64, 16>);
+    return launch(q, out, static_cast<const bf16_t*>(k_pool), static_cast<const bf16_t*>(v_pool), page_table, max_pages, n_seq, n_tokens,
+                  tile_start, item_seq, partial, partial_bytes, n_q, n_kv, n_pool_pages, s);
 }
 
 int laps_launch_attention(const bf16_t* q, bf16_t* out, const void* k_pool, const void* v_pool, bool kv4,
                           const int* page_table, int max_pages, int n_seq, int n_tokens, const int* tile_start,
                           const int* item_seq, float* partial, size_t partial_bytes, int n_q, int n_kv, int hd, int n_pool_pages,
                           hipStream_t s) {
-    if (hd != 64 && hd != 128) {
-        laps_set_error("attention: head_dim %d not supported (64 or 128)", hd);
-        return LAPS_EINVAL;
-    }
-    auto launch = hd == 128 ? (kv4 ? launch_attention<128, true> : launch_attention<128, false>)
-                            : (kv4 ? launch_attention<64, true> : launch_attention<64, false>);
-    return launch(q, out, static_cast<const bf16_t*>(k_pool), static_cast<const bf16_t*>(v_pool), page_table, max_pages, n_seq, n_tokens,
-                  tile_start, item_seq, partial, partial_bytes, n_q, n_kv, n_pool_pages, s);
+    return launch_by_bits(kv4 ? 4 : 16, q, out, k_pool, v_pool, page_table, max_pages, n_seq, n_tokens, tile_start, item_seq, partial, partial_bytes,
+                          n_q, n_kv, hd, n_pool_pages, s);
+}
+
+int laps_launch_attention_kv8(const bf16_t* q, bf16_t* out, const void* k_pool, const void* v_pool, const int* page_table, int max_pages,
+                              int n_seq, int n_tokens, const int* tile_start, const int* item_seq, float* partial, size_t partial_bytes,
+                              int n_q, int n_kv, int hd, int n_pool_pages, hipStream_t s) {
+    return launch_by_bits(8, q, out, k_pool, v_pool, page_table, max_pages, n_seq, n_tokens, tile_start, item_seq, partial, partial_bytes, n_q,
+                          n_kv, hd, n_pool_pages, s);
 }

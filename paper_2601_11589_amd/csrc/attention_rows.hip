@@ -20,6 +20,8 @@
 // 2.3e-3 of the output against 1.6e-3 to 1.7e-3, most of it the output's own rounding), the same as over bf16 pools.
 // Four waves of a workgroup take every fourth pair of pages and add up in LDS.  Few sequences over long keys: a sequence's keys go out
 // in parts of equal length to workgroups of their own, and a second kernel adds those, in order.
+#include "attention_rows.h"
+#include "fp8.h"
 #include "kv4.h"
 
 #include <climits>
@@ -54,15 +56,21 @@ __device__ __forceinline__ int part_steps(int kv_len, int max_pages, int parts, 
 }
 
 // One step's codes and scales as they come from the pools.
-template <int HD>
+template <int HD, bool KV8>
 struct Piece {
     unsigned k[2][HD / 32], ks[2];   // [page]: HD / 4 codes of key i, the dword with their group's scale byte
     u32x4 v[2];                      // eight codes (HD 64: four of them used) of keys 4g .. 4g + 3
     unsigned vs[2];                  // those keys' scale bytes
 };
+template <int HD>
+struct Piece<HD, true> {
+    u32x4 k[2][HD / 64];             // [page]: codes of key i, 16 of every 64
+    u32x4 v[2][HD / 64];             // four head_dim indices of every 64, keys 4g .. 4g + 3 of each a dword
+    unsigned ks[2], vs[2];           // the page's scale bytes, each in a dword of four kv heads'
+};
 
 // NR: blocks of 16 rows that share what is read and unpacked.
-template <int HD, int NR>
+template <int HD, int NR, bool KV8>
 __global__ __launch_bounds__(WAVES * 64, NR == 1 ? 3 : 2) void attn_rows_kernel(
     const bf16_t* __restrict__ q, bf16_t* __restrict__ out, const byte_t* __restrict__ k_pool, const byte_t* __restrict__ v_pool,
     const int* __restrict__ cu, const int* __restrict__ seq_len, const int* __restrict__ prefix_len,
@@ -89,6 +97,7 @@ __global__ __launch_bounds__(WAVES * 64, NR == 1 ? 3 : 2) void attn_rows_kernel(
     const int need = (kv_len + LAPS_PAGE - 1) / LAPS_PAGE, n_pages = need < max_pages ? need : max_pages;
     const int* pt = page_table + (size_t)seq * max_pages;
     const unsigned k_turn = (8 * (HD == 128 ? g : 2 * (i & 1) + (g >> 1)) + 9) & 31;   // right rotation that brings the lane's scale byte up
+    [[maybe_unused]] const int kv8_turn = 8 * (kvh & 3);
     const int v_chunk = HD == 128 ? i : i >> 1, v_group = i / (KV4_GROUP / DL), o_group = g * 4 * DL / KV4_GROUP;
 
     for (int rb = rb0; rb * ROWS < n_rows; rb += row_blocks) {
@@ -102,7 +111,7 @@ __global__ __launch_bounds__(WAVES * 64, NR == 1 ? 3 : 2) void attn_rows_kernel(
             limit[a] = r.H + tq;
             const u32x4* qp = reinterpret_cast<const u32x4*>(q + (size_t)(r.rs + tq) * n_q * HD + (size_t)(kvh * G + rc - tq * G) * HD);
 #pragma unroll
-            for (int kk = 0; kk < KS; ++kk) qf[a][kk] = __builtin_bit_cast(bf16x8, qp[g * KS + kk]);
+            for (int kk = 0; kk < KS; ++kk) qf[a][kk] = __builtin_bit_cast(bf16x8, qp[KV8 ? kk / 2 * 8 + g * 2 + kk % 2 : g * KS + kk]);
         }
         f32x4 o[NR][DL];
         float m_run[NR], l_run[NR];   // reference in log2 units (the same in the four lanes of a row), this lane's sum
@@ -131,38 +140,54 @@ __global__ __launch_bounds__(WAVES * 64, NR == 1 ? 3 : 2) void attn_rows_kernel(
         // Up to 16 rows a sequence: keys are read once and past the caches, 2.3 GB 418 -> 378 us (6.0 TB/s; 280 MB that the memory-side cache
         // held from the call before 52 -> 58).  More rows: other blocks of theirs read the same keys.
         auto codes = [](const auto* from) { return NR == 1 ? __builtin_nontemporal_load(from) : *from; };
-        auto load = [&](int n, Piece<HD>& x) {
+        auto load = [&](int n, Piece<HD, KV8>& x) {
             if ((n & 31) == 0) fetch_ids(n);
 #pragma unroll
             for (int p = 0; p < 2; ++p) {
                 const int page = __builtin_amdgcn_readlane(ids, 2 * (n & 31) + p);
-                const size_t at = ((size_t)page * n_kv + kvh) * BLOCK;
-                const byte_t *kb = k_pool + at, *vb = v_pool + at;
-                if constexpr (HD == 128) {
-                    const u32x4 w = codes(reinterpret_cast<const u32x4*>(kb) + i * 4 + g);
+                if constexpr (KV8) {
+                    const size_t at = (size_t)page * kv8_page(n_kv, HD);
+                    const byte_t *kb = k_pool + at, *vb = v_pool + at;
+                    const int own = kvh * (kv8_codes(HD) / 16), scales = n_kv * (kv8_codes(HD) / 4) + kvh / 4;
 #pragma unroll
-                    for (int kk = 0; kk < 4; ++kk) x.k[p][kk] = w[kk];
+                    for (int u = 0; u < HD / 64; ++u) {
+                        x.k[p][u] = codes(reinterpret_cast<const u32x4*>(kb) + own + i * (HD / 16) + u * 4 + g);
+                        x.v[p][u] = codes(reinterpret_cast<const u32x4*>(vb) + own + (16 * u + i) * 4 + g);
+                    }
+                    x.ks[p] = reinterpret_cast<const unsigned*>(kb)[scales];
+                    x.vs[p] = reinterpret_cast<const unsigned*>(vb)[scales];
                 } else {
-                    const u32x2 w = codes(reinterpret_cast<const u32x2*>(kb) + i * 4 + g);
-                    x.k[p][0] = w.x;
-                    x.k[p][1] = w.y;
+                    const size_t at = ((size_t)page * n_kv + kvh) * BLOCK;
+                    const byte_t *kb = k_pool + at, *vb = v_pool + at;
+                    if constexpr (HD == 128) {
+                        const u32x4 w = codes(reinterpret_cast<const u32x4*>(kb) + i * 4 + g);
+#pragma unroll
+                        for (int kk = 0; kk < 4; ++kk) x.k[p][kk] = w[kk];
+                    } else {
+                        const u32x2 w = codes(reinterpret_cast<const u32x2*>(kb) + i * 4 + g);
+                        x.k[p][0] = w.x;
+                        x.k[p][1] = w.y;
+                    }
+                    x.ks[p] = reinterpret_cast<const unsigned*>(kb + CODES)[HD == 128 ? i : i >> 1];
+                    x.v[p] = codes(reinterpret_cast<const u32x4*>(vb) + v_chunk * 4 + g);
+                    x.vs[p] = reinterpret_cast<const unsigned*>(vb + CODES)[v_group * 4 + g];
                 }
-                x.ks[p] = reinterpret_cast<const unsigned*>(kb + CODES)[HD == 128 ? i : i >> 1];
-                x.v[p] = codes(reinterpret_cast<const u32x4*>(vb) + v_chunk * 4 + g);
-                x.vs[p] = reinterpret_cast<const unsigned*>(vb + CODES)[v_group * 4 + g];
             }
         };
-        auto compute = [&](int n, Piece<HD>& x) {
+        auto compute = [&](int n, Piece<HD, KV8>& x) {
             const int key0 = (s_begin + n * WAVES) * STEP;
             f32x4 s[NR][2];
 #pragma unroll
             for (int p = 0; p < 2; ++p) {
-                const float ks = __uint_as_float(__builtin_amdgcn_alignbit(x.ks[p], x.ks[p], k_turn));   // the byte to bits 23 to 30
+                const float ks = KV8 ? fp8_scale(x.ks[p] >> kv8_turn & 255u)
+                                     : __uint_as_float(__builtin_amdgcn_alignbit(x.ks[p], x.ks[p], k_turn));   // the byte to bits 23 to 30
 #pragma unroll
                 for (int a = 0; a < NR; ++a) s[a][p] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int kk = 0; kk < KS; ++kk) {
-                    const bf16x8 kf = __builtin_bit_cast(bf16x8, kv4_eight(x.k[p][kk], ks));
+                    bf16x8 kf;
+                    if constexpr (KV8) kf = __builtin_bit_cast(bf16x8, fp8_eight(x.k[p][kk / 2][kk % 2 * 2], x.k[p][kk / 2][kk % 2 * 2 + 1], ks));
+                    else kf = __builtin_bit_cast(bf16x8, kv4_eight(x.k[p][kk], ks));
 #pragma unroll
                     for (int a = 0; a < NR; ++a) s[a][p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[a][kk], s[a][p], 0, 0, 0);
                 }
@@ -178,11 +203,19 @@ __global__ __launch_bounds__(WAVES * 64, NR == 1 ? 3 : 2) void attn_rows_kernel(
                             if (k4 + e > limit[a]) s[a][p][e] = -INFINITY;   // whatever it was, NaN included
                         // V of a key that a row does not see has weight zero, which a NaN would survive: slots past the sequence's end
                         // hold anything, and a NaN group of a key before it shows in the rows that see it only
-                        const unsigned byte = (x.vs[p] >> (8 * e)) & 255u;
-                        if (k4 + e >= kv_len || byte == 255u) {
-                            if (k4 + e < kv_len) nan_key = k4 + e < nan_key ? k4 + e : nan_key;
-                            x.v[p][e] = 0u;
-                            x.vs[p] &= ~(255u << (8 * e));
+                        if constexpr (KV8) {   // a token's head is NaN as a whole or not at all
+                            if (k4 + e >= kv_len || (x.v[p][0].x >> (8 * e) & 127u) == 127u) {
+                                if (k4 + e < kv_len) nan_key = k4 + e < nan_key ? k4 + e : nan_key;
+#pragma unroll
+                                for (int u = 0; u < HD / 64; ++u) x.v[p][u] &= ~(255u << (8 * e));
+                            }
+                        } else {
+                            const unsigned byte = (x.vs[p] >> (8 * e)) & 255u;
+                            if (k4 + e >= kv_len || byte == 255u) {
+                                if (k4 + e < kv_len) nan_key = k4 + e < nan_key ? k4 + e : nan_key;
+                                x.v[p][e] = 0u;
+                                x.vs[p] &= ~(255u << (8 * e));
+                            }
                         }
                     }
                 }
@@ -232,42 +265,53 @@ __global__ __launch_bounds__(WAVES * 64, NR == 1 ? 3 : 2) void attn_rows_kernel(
             }
 #pragma unroll
             for (int a = 0; a < NR; ++a) l_run[a] += sum[a];
-            // codes of one head_dim pair of the eight keys, then the keys side by side
-            auto pair_of_keys = [&](auto B) {
-                constexpr int b = decltype(B)::value;
-                unsigned w[8];
+            if constexpr (KV8) {   // the keys lie side by side already
+                const float vs0 = fp8_scale(x.vs[0] >> kv8_turn & 255u), vs1 = fp8_scale(x.vs[1] >> kv8_turn & 255u);
 #pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                    auto word = [&](int e) { return HD == 128 ? x.v[p][e] : x.v[p][e] >> (16 * (i & 1)); };
-                    w[4 * p + 0] = kv4_pair<b>(word(0), kv4_scale<0>(x.vs[p]));
-                    w[4 * p + 1] = kv4_pair<b>(word(1), kv4_scale<1>(x.vs[p]));
-                    w[4 * p + 2] = kv4_pair<b>(word(2), kv4_scale<2>(x.vs[p]));
-                    w[4 * p + 3] = kv4_pair<b>(word(3), kv4_scale<3>(x.vs[p]));
-                }
-                u32x4 lo, hi;
+                for (int j = 0; j < DL; ++j) {
+                    const u32x2 lo = fp8_four(x.v[0][j / 4][j % 4], vs0), hi = fp8_four(x.v[1][j / 4][j % 4], vs1);
+                    const bf16x8 vf = __builtin_bit_cast(bf16x8, u32x4{lo.x, lo.y, hi.x, hi.y});
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    lo[k] = __builtin_amdgcn_perm(w[2 * k + 1], w[2 * k], 0x05040100u);
-                    hi[k] = __builtin_amdgcn_perm(w[2 * k + 1], w[2 * k], 0x07060302u);
+                    for (int a = 0; a < NR; ++a) o[a][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[a], o[a][j], 0, 0, 0);
                 }
+            } else {
+                // codes of one head_dim pair of the eight keys, then the keys side by side
+                auto pair_of_keys = [&](auto B) {
+                    constexpr int b = decltype(B)::value;
+                    unsigned w[8];
 #pragma unroll
-                for (int a = 0; a < NR; ++a) {
-                    o[a][2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), pf[a], o[a][2 * b], 0, 0, 0);
-                    o[a][2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), pf[a], o[a][2 * b + 1], 0, 0, 0);
+                    for (int p = 0; p < 2; ++p) {
+                        auto word = [&](int e) { return HD == 128 ? x.v[p][e] : x.v[p][e] >> (16 * (i & 1)); };
+                        w[4 * p + 0] = kv4_pair<b>(word(0), kv4_scale<0>(x.vs[p]));
+                        w[4 * p + 1] = kv4_pair<b>(word(1), kv4_scale<1>(x.vs[p]));
+                        w[4 * p + 2] = kv4_pair<b>(word(2), kv4_scale<2>(x.vs[p]));
+                        w[4 * p + 3] = kv4_pair<b>(word(3), kv4_scale<3>(x.vs[p]));
+                    }
+                    u32x4 lo, hi;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        lo[k] = __builtin_amdgcn_perm(w[2 * k + 1], w[2 * k], 0x05040100u);
+                        hi[k] = __builtin_amdgcn_perm(w[2 * k + 1], w[2 * k], 0x07060302u);
+                    }
+#pragma unroll
+                    for (int a = 0; a < NR; ++a) {
+                        o[a][2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), pf[a], o[a][2 * b], 0, 0, 0);
+                        o[a][2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), pf[a], o[a][2 * b + 1], 0, 0, 0);
+                    }
+                };
+                pair_of_keys(std::integral_constant<int, 0>{});
+                pair_of_keys(std::integral_constant<int, 1>{});
+                if constexpr (HD == 128) {
+                    pair_of_keys(std::integral_constant<int, 2>{});
+                    pair_of_keys(std::integral_constant<int, 3>{});
                 }
-            };
-            pair_of_keys(std::integral_constant<int, 0>{});
-            pair_of_keys(std::integral_constant<int, 1>{});
-            if constexpr (HD == 128) {
-                pair_of_keys(std::integral_constant<int, 2>{});
-                pair_of_keys(std::integral_constant<int, 3>{});
             }
         };
         // The next step is on its way while one is worked on; two buffers in turn.  Past the last step the last one is loaded again:
         // with a branch round the loads every wait would be for all of them.
         if (n_steps > 0) {
-            Piece<HD> x, y;
-            auto load_at = [&](int n, Piece<HD>& to) { load(n < n_steps ? n : n_steps - 1, to); };
+            Piece<HD, KV8> x, y;
+            auto load_at = [&](int n, Piece<HD, KV8>& to) { load(n < n_steps ? n : n_steps - 1, to); };
             load_at(0, x);
 #pragma unroll
             for (int a = 0; a < NR; ++a)
@@ -288,7 +332,7 @@ __global__ __launch_bounds__(WAVES * 64, NR == 1 ? 3 : 2) void attn_rows_kernel(
         // ---- NaN groups of keys that not every row sees
         nan_key = min(nan_key, __shfl_xor(nan_key, 16, 64));
         nan_key = min(nan_key, __shfl_xor(nan_key, 32, 64));
-        const int nan_from = __shfl(nan_key, o_group * (KV4_GROUP / DL), 64);
+        const int nan_from = KV8 ? nan_key : __shfl(nan_key, o_group * (KV4_GROUP / DL), 64);
 #pragma unroll
         for (int a = 0; a < NR; ++a) {
             if (rb * ROWS + 16 * a >= n_rows) break;
@@ -296,7 +340,7 @@ __global__ __launch_bounds__(WAVES * 64, NR == 1 ? 3 : 2) void attn_rows_kernel(
 #pragma unroll
                 for (int j = 0; j < DL; ++j) o[a][j] += __builtin_nanf("");
             }
-            // ---- the four waves' results: lane (i, g) holds row i, head_dim indices 4 DL g + DL e + j
+            // ---- the four waves' results: lane (i, g) holds row i, head_dim indices 4 DL g + DL e + j (8 bits: 64 (j / 4) + 16 g + 4 e + j % 4)
             l_run[a] += __shfl_xor(l_run[a], 16, 64);
             l_run[a] += __shfl_xor(l_run[a], 32, 64);
             __syncthreads();   // the rows before are read
@@ -304,7 +348,7 @@ __global__ __launch_bounds__(WAVES * 64, NR == 1 ? 3 : 2) void attn_rows_kernel(
             for (int e = 0; e < 4; ++e)
 #pragma unroll
                 for (int j = 0; j < DL; j += 4)
-                    *reinterpret_cast<f32x4*>(&red_o[wave][i][(4 * g + e) * DL + j]) = f32x4{o[a][j][e], o[a][j + 1][e], o[a][j + 2][e], o[a][j + 3][e]};
+                    *reinterpret_cast<f32x4*>(&red_o[wave][i][KV8 ? 16 * j + 16 * g + 4 * e : (4 * g + e) * DL + j]) = f32x4{o[a][j][e], o[a][j + 1][e], o[a][j + 2][e], o[a][j + 3][e]};
             if (g == 0) {
                 red_ml[wave][0][i] = m_run[a];
                 red_ml[wave][1][i] = l_run[a];
@@ -473,11 +517,11 @@ __global__ __launch_bounds__(FEW_THREADS) void attn_rows_merge_few_kernel(bf16_t
     }
 }
 
-template <int HD>
-int launch_rows(const Kv4Attn& a, const Kv4RowsPlan& p, float* part, hipStream_t s) {
+template <int HD, bool KV8>
+int launch_rows(const RowsAttn& a, const RowsPlan& p, float* part, hipStream_t s) {
     const float scale_log2e = 1.4426950408889634f / sqrtf((float)HD);
     float* part_ml = part ? part + (size_t)a.n_tokens * a.n_q * p.parts * HD : nullptr;
-    auto kern = p.row_tiles == 1 ? attn_rows_kernel<HD, 1> : attn_rows_kernel<HD, 2>;
+    auto kern = p.row_tiles == 1 ? attn_rows_kernel<HD, 1, KV8> : attn_rows_kernel<HD, 2, KV8>;
     hipLaunchKernelGGL(kern, dim3((a.n_seq * p.parts * p.row_blocks + 7) / 8 * 8 * a.n_kv), dim3(WAVES * 64), 0, s, a.q, a.out, a.k_pool,
                        a.v_pool, a.cu, a.seq_len, a.prefix_len, a.page_table, a.max_pages, a.n_seq, a.n_tokens, a.n_q, a.n_kv, a.n_pool_pages,
                        p.row_blocks, p.parts, p.min_parts, scale_log2e, part, part_ml);
@@ -508,12 +552,12 @@ int launch_rows(const Kv4Attn& a, const Kv4RowsPlan& p, float* part, hipStream_t
 // split.  And rows count by their mean: a long turn among single tokens is walked block after block by the few workgroups of
 // a sequence (32B, 95 tokens over 512 to 8100 keys 98 us, a turn of 350 over 4000 65, both in one call 1620, in blocks 363; 7B,
 // 127 tokens 72, a turn of 900 100, both 3008, in blocks 334).
-bool laps_kv4_takes_rows(int n_seq, int n_tokens, int n_q, int n_kv) {
+bool laps_attn_takes_rows(int bits, int n_seq, int n_tokens, int n_q, int n_kv) {
     const long rows = (long)n_tokens * (n_q / n_kv), blocks = (rows + 32L * n_seq - 1) / (32L * n_seq);
     return rows <= 16L * n_seq || blocks * n_seq * n_kv <= 1024;
 }
 
-Kv4RowsPlan laps_kv4_rows_plan(int n_seq, int n_tokens, int n_q, int n_kv, int max_pages) {
+RowsPlan laps_attn_rows_plan(int bits, int n_seq, int n_tokens, int n_q, int n_kv, int max_pages) {
     const long rows = (long)n_tokens * (n_q / n_kv);
     const int tiles = rows > 16L * n_seq ? 2 : 1;
     long blocks = (rows + 16L * tiles * n_seq - 1) / (16L * tiles * n_seq);
@@ -540,10 +584,11 @@ Kv4RowsPlan laps_kv4_rows_plan(int n_seq, int n_tokens, int n_q, int n_kv, int m
     return {tiles, (int)blocks, (int)(parts > min_parts ? parts : min_parts), (int)min_parts};
 }
 
-size_t laps_kv4_rows_bytes(const Kv4RowsPlan& p, int n_tokens, int n_q, int hd) {
+size_t laps_attn_rows_bytes(const RowsPlan& p, int n_tokens, int n_q, int hd) {
     return p.parts > 1 ? (size_t)n_tokens * n_q * p.parts * (hd + 2) * sizeof(float) : 0;
 }
 
-int laps_launch_kv4_rows(const Kv4Attn& a, const Kv4RowsPlan& p, float* partial, hipStream_t s) {
-    return a.hd == 128 ? launch_rows<128>(a, p, partial, s) : launch_rows<64>(a, p, partial, s);
+int laps_launch_attn_rows(const RowsAttn& a, const RowsPlan& p, float* partial, hipStream_t s) {
+    auto launch = a.hd == 128 ? (a.bits == 8 ? launch_rows<128, true> : launch_rows<128, false>) : (a.bits == 8 ? launch_rows<64, true> : launch_rows<64, false>);
+    return launch(a, p, partial, s);
 }

@@ -9,6 +9,8 @@
 #include <new>
 #include <vector>
 
+#include "attention_rows.h"
+#include "fp8.h"
 #include "kv4.h"
 #include "laps_internal.h"
 
@@ -600,18 +602,28 @@ extern "C" size_t laps_kv4_block_bytes(int32_t head_dim) {
     return head_dim == 64 || head_dim == 128 ? (size_t)kv4_block(head_dim) : 0;
 }
 
-static int kv4_move(bool scatter, laps_ctx* c, int n_seq, int n_tokens, const int* cu, const int* start_pos, const int* pt,
-                    int max_pages, void* k_tok, void* v_tok, void* k_pool, void* v_pool, void* stream) {
-    if (!c || n_seq < 1 || n_tokens < 0 || !cu || !start_pos || !pt || max_pages < 1 || max_pages > LAPS_KV4_MAX_PAGES || !k_pool || !v_pool ||
+extern "C" size_t laps_kv8_page_bytes(int32_t n_kv_heads, int32_t head_dim) {
+    return n_kv_heads >= 1 && (head_dim == 64 || head_dim == 128) ? kv8_page(n_kv_heads, head_dim) : 0;
+}
+
+// Checks of a move between token-major rows and quantised pools.
+static int check_move(const char* who, const laps_ctx* c, int n_seq, int n_tokens, const int* cu, const int* start_pos, const int* pt,
+                      int max_pages, const void* k_tok, const void* v_tok, const void* k_pool, const void* v_pool) {
+    if (!c || n_seq < 1 || n_tokens < 0 || !cu || !start_pos || !pt || max_pages < 1 || max_pages > LAPS_KVQ_MAX_PAGES || !k_pool || !v_pool ||
         (n_tokens > 0 && (!k_tok || !v_tok))) {
-        laps_set_error("kv4 move: NULL pointer or bad size");
+        laps_set_error("%s: NULL pointer or bad size", who);
         return LAPS_EINVAL;
     }
     if (((uintptr_t)k_tok | (uintptr_t)v_tok | (uintptr_t)k_pool | (uintptr_t)v_pool) & 15) {
-        laps_set_error("kv4 move: K/V rows and pools must be 16-byte aligned");
+        laps_set_error("%s: K/V rows and pools must be 16-byte aligned", who);
         return LAPS_EINVAL;
     }
-    LAPS_TRY(check_current_device(c, "kv4 move"));
+    return check_current_device(c, who);
+}
+
+static int kv4_move(bool scatter, laps_ctx* c, int n_seq, int n_tokens, const int* cu, const int* start_pos, const int* pt,
+                    int max_pages, void* k_tok, void* v_tok, void* k_pool, void* v_pool, void* stream) {
+    LAPS_TRY(check_move("kv4 move", c, n_seq, n_tokens, cu, start_pos, pt, max_pages, k_tok, v_tok, k_pool, v_pool));
     return laps_launch_kv4_move(scatter, n_seq, n_tokens, cu, start_pos, pt, max_pages, k_tok, v_tok, k_pool, v_pool,
                                 c->cfg.n_kv_heads, c->cfg.head_dim, kv4_pool_pages(c), static_cast<hipStream_t>(stream));
 }
@@ -630,8 +642,33 @@ extern "C" int laps_kv4_gather(laps_ctx* c, int32_t n_seq, int32_t n_tokens, con
                     const_cast<void*>(v_pool), stream);
 }
 
-// Workspace of the block kernels: lengths, work items, partial results.
-static WsLayout kv4_layout(int n_seq, int n_tokens, int n_q, int n_kv, int hd, int max_pages) {
+static int kv8_move(bool scatter, laps_ctx* c, int n_seq, int n_tokens, const int* cu, const int* start_pos, const int* pt, int max_pages,
+                    int n_pages, void* k_tok, void* v_tok, void* k_pool, void* v_pool, void* stream) {
+    LAPS_TRY(check_move("kv8 move", c, n_seq, n_tokens, cu, start_pos, pt, max_pages, k_tok, v_tok, k_pool, v_pool));
+    if (n_pages < 1) {
+        laps_set_error("kv8 move: the pools hold %d pages", n_pages);
+        return LAPS_EINVAL;
+    }
+    return laps_launch_kv8_move(scatter, n_seq, n_tokens, cu, start_pos, pt, max_pages, k_tok, v_tok, k_pool, v_pool,
+                                c->cfg.n_kv_heads, c->cfg.head_dim, n_pages, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int laps_kv8_scatter(laps_ctx* c, int32_t n_seq, int32_t n_tokens, const int32_t* cu, const int32_t* start_pos,
+                                const int32_t* pt, int32_t max_pages, int32_t n_pages, const void* k_src, const void* v_src,
+                                void* k_pool, void* v_pool, void* stream) {
+    return kv8_move(true, c, n_seq, n_tokens, cu, start_pos, pt, max_pages, n_pages, const_cast<void*>(k_src), const_cast<void*>(v_src),
+                    k_pool, v_pool, stream);
+}
+
+extern "C" int laps_kv8_gather(laps_ctx* c, int32_t n_seq, int32_t n_tokens, const int32_t* cu, const int32_t* start_pos,
+                               const int32_t* pt, int32_t max_pages, int32_t n_pages, const void* k_pool, const void* v_pool,
+                               void* k_dst, void* v_dst, void* stream) {
+    return kv8_move(false, c, n_seq, n_tokens, cu, start_pos, pt, max_pages, n_pages, k_dst, v_dst, const_cast<void*>(k_pool),
+                    const_cast<void*>(v_pool), stream);
+}
+
+// ---- attention over quantised pools.  Workspace of the block kernels: lengths, work items, partial results.
+static WsLayout kvq_layout(int n_seq, int n_tokens, int n_q, int n_kv, int hd, int max_pages) {
     WsLayout w = {};
     const int group = n_q / n_kv;
     w.tile_start = align256((size_t)n_seq * 4);
@@ -641,28 +678,24 @@ static WsLayout kv4_layout(int n_seq, int n_tokens, int n_q, int n_kv, int hd, i
     return w;
 }
 
-static size_t kv4_workspace_bytes(int n_seq, int n_tokens, int n_q, int n_kv, int hd, int max_pages) {
-    if (n_seq < 1 || n_tokens < 1 || max_pages < 1 || max_pages > LAPS_KV4_MAX_PAGES || (long)n_seq * n_q > LAPS_KV4_MAX_SEQ_HEADS) return 0;
-    if (!laps_kv4_takes_rows(n_seq, n_tokens, n_q, n_kv)) return kv4_layout(n_seq, n_tokens, n_q, n_kv, hd, max_pages).total;
-    return align256(laps_kv4_rows_bytes(laps_kv4_rows_plan(n_seq, n_tokens, n_q, n_kv, max_pages), n_tokens, n_q, hd) + 1);
+static size_t kvq_workspace_bytes(int bits, int n_seq, int n_tokens, int n_q, int n_kv, int hd, int max_pages) {
+    if (n_seq < 1 || n_tokens < 1 || max_pages < 1 || max_pages > LAPS_KVQ_MAX_PAGES || (long)n_seq * n_q > LAPS_KVQ_MAX_SEQ_HEADS) return 0;
+    if (!laps_attn_takes_rows(bits, n_seq, n_tokens, n_q, n_kv)) return kvq_layout(n_seq, n_tokens, n_q, n_kv, hd, max_pages).total;
+    return align256(laps_attn_rows_bytes(laps_attn_rows_plan(bits, n_seq, n_tokens, n_q, n_kv, max_pages), n_tokens, n_q, hd) + 1);
 }
 
-extern "C" size_t laps_attention_kv4_workspace_bytes(const laps_ctx* c, int32_t n_seq, int32_t n_tokens, int32_t max_pages) {
-    return c ? kv4_workspace_bytes(n_seq, n_tokens, c->cfg.n_q_heads, c->cfg.n_kv_heads, c->cfg.head_dim, max_pages) : 0;
-}
-
-extern "C" int laps_attention_kv4_plan_info(int32_t n_seq, int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
-                                            int32_t max_pages, int64_t* out) {
+static int kvq_plan_info(const char* who, int bits, int n_seq, int n_tokens, int n_q_heads, int n_kv_heads, int head_dim, int max_pages,
+                         int64_t* out) {
     size_t bytes = 0;
     if (out && n_q_heads >= 1 && n_kv_heads >= 1 && n_q_heads % n_kv_heads == 0 && (head_dim == 64 || head_dim == 128))
-        bytes = kv4_workspace_bytes(n_seq, n_tokens, n_q_heads, n_kv_heads, head_dim, max_pages);
+        bytes = kvq_workspace_bytes(bits, n_seq, n_tokens, n_q_heads, n_kv_heads, head_dim, max_pages);
     if (bytes == 0) {
-        laps_set_error("attention_kv4_plan_info: NULL output or unsupported shape");
+        laps_set_error("%s: NULL output or unsupported shape", who);
         return LAPS_EINVAL;
     }
     out[5] = (int64_t)bytes;
-    if (laps_kv4_takes_rows(n_seq, n_tokens, n_q_heads, n_kv_heads)) {
-        const Kv4RowsPlan p = laps_kv4_rows_plan(n_seq, n_tokens, n_q_heads, n_kv_heads, max_pages);
+    if (laps_attn_takes_rows(bits, n_seq, n_tokens, n_q_heads, n_kv_heads)) {
+        const RowsPlan p = laps_attn_rows_plan(bits, n_seq, n_tokens, n_q_heads, n_kv_heads, max_pages);
         out[0] = 16 * p.row_tiles;
         out[1] = p.row_blocks;
         out[2] = p.parts;
@@ -672,7 +705,7 @@ extern "C" int laps_attention_kv4_plan_info(int32_t n_seq, int32_t n_tokens, int
     }
     int rows = 0, items = 0, split = 0, min_tiles = 0;
     const int group = n_q_heads / n_kv_heads;
-    const WsLayout L = kv4_layout(n_seq, n_tokens, n_q_heads, n_kv_heads, head_dim, max_pages);
+    const WsLayout L = kvq_layout(n_seq, n_tokens, n_q_heads, n_kv_heads, head_dim, max_pages);
     laps_attn_plan(n_seq, n_tokens, group, n_kv_heads, max_pages, &rows, &items, &split, &min_tiles);
     out[0] = rows;
     out[1] = items;
@@ -681,47 +714,196 @@ extern "C" int laps_attention_kv4_plan_info(int32_t n_seq, int32_t n_tokens, int
     return LAPS_OK;
 }
 
-extern "C" int laps_attention_kv4(laps_ctx* c, int32_t n_seq, int32_t n_tokens, const int32_t* cu, const int32_t* seq_len,
-                                  const int32_t* prefix_len, const int32_t* pt, int32_t max_pages, const void* k_pool,
-                                  const void* v_pool, const void* q, void* out, void* ws, size_t ws_bytes, void* stream) {
+static int attention_kvq(const char* who, int bits, laps_ctx* c, int n_seq, int n_tokens, const int* cu, const int* seq_len,
+                         const int* prefix_len, const int* pt, int max_pages, int n_pages, const void* k_pool, const void* v_pool,
+                         const void* q, void* out, void* ws, size_t ws_bytes, void* stream) {
     if (!c || n_seq < 1 || n_tokens < 1 || !cu || !prefix_len || !pt || max_pages < 1 || !k_pool || !v_pool || !q || !out || !ws) {
-        laps_set_error("attention_kv4: NULL pointer or bad size");
+        laps_set_error("%s: NULL pointer or bad size", who);
         return LAPS_EINVAL;
     }
-    const size_t need = laps_attention_kv4_workspace_bytes(c, n_seq, n_tokens, max_pages);
+    const laps_model_cfg& cf = c->cfg;
+    const size_t need = kvq_workspace_bytes(bits, n_seq, n_tokens, cf.n_q_heads, cf.n_kv_heads, cf.head_dim, max_pages);
     if (need == 0) {
-        laps_set_error("attention_kv4: %d sequences of %d query heads or page tables of %d pages are too many", n_seq,
-                       c->cfg.n_q_heads, max_pages);
+        laps_set_error("%s: %d sequences of %d query heads or page tables of %d pages are too many", who, n_seq, cf.n_q_heads, max_pages);
         return LAPS_EINVAL;
     }
     if ((((uintptr_t)k_pool | (uintptr_t)v_pool | (uintptr_t)q | (uintptr_t)out) & 15) || ((uintptr_t)ws & 255)) {
-        laps_set_error("attention_kv4: pools, q and out must be 16-byte aligned, the workspace 256-byte");
+        laps_set_error("%s: pools, q and out must be 16-byte aligned, the workspace 256-byte", who);
         return LAPS_EINVAL;
     }
-    LAPS_TRY(check_current_device(c, "attention_kv4"));
+    LAPS_TRY(check_current_device(c, who));
     if (ws_bytes < need) {
-        laps_set_error("attention_kv4: workspace too small (%zu < %zu bytes)", ws_bytes, need);
+        laps_set_error("%s: workspace too small (%zu < %zu bytes)", who, ws_bytes, need);
         return LAPS_ENOMEM;
     }
-    const laps_model_cfg& cf = c->cfg;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (laps_kv4_takes_rows(n_seq, n_tokens, cf.n_q_heads, cf.n_kv_heads)) {
-        const Kv4Attn a = {static_cast<const bf16_t*>(q), static_cast<bf16_t*>(out), static_cast<const unsigned char*>(k_pool),
-                           static_cast<const unsigned char*>(v_pool), cu, seq_len, prefix_len, pt, n_seq, n_tokens, max_pages,
-                           kv4_pool_pages(c), cf.n_q_heads, cf.n_kv_heads, cf.head_dim};
-        const Kv4RowsPlan p = laps_kv4_rows_plan(n_seq, n_tokens, a.n_q, a.n_kv, max_pages);
-        return laps_launch_kv4_rows(a, p, p.parts > 1 ? static_cast<float*>(ws) : nullptr, s);
+    if (laps_attn_takes_rows(bits, n_seq, n_tokens, cf.n_q_heads, cf.n_kv_heads)) {
+        const RowsAttn a = {static_cast<const bf16_t*>(q), static_cast<bf16_t*>(out), static_cast<const unsigned char*>(k_pool),
+                            static_cast<const unsigned char*>(v_pool), cu, seq_len, prefix_len, pt, n_seq, n_tokens, max_pages,
+                            n_pages, cf.n_q_heads, cf.n_kv_heads, cf.head_dim, bits};
+        const RowsPlan p = laps_attn_rows_plan(bits, n_seq, n_tokens, a.n_q, a.n_kv, max_pages);
+        return laps_launch_attn_rows(a, p, p.parts > 1 ? static_cast<float*>(ws) : nullptr, s);
     }
-    const WsLayout L = kv4_layout(n_seq, n_tokens, cf.n_q_heads, cf.n_kv_heads, cf.head_dim, max_pages);
+    const WsLayout L = kvq_layout(n_seq, n_tokens, cf.n_q_heads, cf.n_kv_heads, cf.head_dim, max_pages);
     unsigned char* w8 = static_cast<unsigned char*>(ws);
     const BatchDesc b{n_seq, n_tokens, cu, seq_len, prefix_len, pt, max_pages};
     BeginArgs begin = begin_args(c, b, w8, L);
     begin.d = 0;   // no rows: the smaller of its kernels, 1 us less
     LAPS_TRY(laps_launch_begin(begin, s));
-    return laps_launch_attention(static_cast<const bf16_t*>(q), static_cast<bf16_t*>(out), k_pool, v_pool, true, pt, max_pages, n_seq,
-                                 n_tokens, reinterpret_cast<int*>(w8 + L.tile_start), reinterpret_cast<int*>(w8 + L.item_seq),
-                                 reinterpret_cast<float*>(w8 + L.partial), L.total - L.partial, cf.n_q_heads, cf.n_kv_heads,
-                                 cf.head_dim, kv4_pool_pages(c), s);
+    const int *tile_start = reinterpret_cast<int*>(w8 + L.tile_start), *item_seq = reinterpret_cast<int*>(w8 + L.item_seq);
+    float* partial = reinterpret_cast<float*>(w8 + L.partial);
+    const size_t partial_bytes = L.total - L.partial;
+    const bf16_t* qp = static_cast<const bf16_t*>(q);
+    bf16_t* op = static_cast<bf16_t*>(out);
+    if (bits == 8)
+        return laps_launch_attention_kv8(qp, op, k_pool, v_pool, pt, max_pages, n_seq, n_tokens, tile_start, item_seq, partial, partial_bytes,
+                                         cf.n_q_heads, cf.n_kv_heads, cf.head_dim, n_pages, s);
+    return laps_launch_attention(qp, op, k_pool, v_pool, true, pt, max_pages, n_seq, n_tokens, tile_start, item_seq, partial, partial_bytes,
+                                 cf.n_q_heads, cf.n_kv_heads, cf.head_dim, n_pages, s);
+}
+
+extern "C" size_t laps_attention_kv4_workspace_bytes(const laps_ctx* c, int32_t n_seq, int32_t n_tokens, int32_t max_pages) {
+    return c ? kvq_workspace_bytes(4, n_seq, n_tokens, c->cfg.n_q_heads, c->cfg.n_kv_heads, c->cfg.head_dim, max_pages) : 0;
+}
+
+extern "C" int laps_attention_kv4_plan_info(int32_t n_seq, int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                            int32_t max_pages, int64_t* out) {
+    return kvq_plan_info("attention_kv4_plan_info", 4, n_seq, n_tokens, n_q_heads, n_kv_heads, head_dim, max_pages, out);
+}
+
+extern "C" int laps_attention_kv4(laps_ctx* c, int32_t n_seq, int32_t n_tokens, const int32_t* cu, const int32_t* seq_len,
+                                  const int32_t* prefix_len, const int32_t* pt, int32_t max_pages, const void* k_pool,
+                                  const void* v_pool, const void* q, void* out, void* ws, size_t ws_bytes, void* stream) {
+    return attention_kvq("attention_kv4", 4, c, n_seq, n_tokens, cu, seq_len, prefix_len, pt, max_pages, c ? kv4_pool_pages(c) : 0, k_pool,
+                         v_pool, q, out, ws, ws_bytes, stream);
+}
+
+extern "C" size_t laps_attention_kv8_workspace_bytes(const laps_ctx* c, int32_t n_seq, int32_t n_tokens, int32_t max_pages) {
+    return c ? kvq_workspace_bytes(8, n_seq, n_tokens, c->cfg.n_q_heads, c->cfg.n_kv_heads, c->cfg.head_dim, max_pages) : 0;
+}
+
+extern "C" int laps_attention_kv8_plan_info(int32_t n_seq, int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                            int32_t max_pages, int64_t* out) {
+    return kvq_plan_info("attention_kv8_plan_info", 8, n_seq, n_tokens, n_q_heads, n_kv_heads, head_dim, max_pages, out);
+}
+
+extern "C" int laps_attention_kv8(laps_ctx* c, int32_t n_seq, int32_t n_tokens, const int32_t* cu, const int32_t* seq_len,
+                                  const int32_t* prefix_len, const int32_t* pt, int32_t max_pages, int32_t n_pages, const void* k_pool,
+                                  const void* v_pool, const void* q, void* out, void* ws, size_t ws_bytes, void* stream) {
+    if (n_pages < 1) {
+        laps_set_error("attention_kv8: the pools hold %d pages", n_pages);
+        return LAPS_EINVAL;
+    }
+    return attention_kvq("attention_kv8", 8, c, n_seq, n_tokens, cu, seq_len, prefix_len, pt, max_pages, n_pages, k_pool, v_pool, q, out, ws,
+                         ws_bytes, stream);
+}
+
+// ---- 8-bit matrices
+constexpr int FP8_MAX_K = 1 << 22, FP8_MAX_ROWS = 1 << 24;   // 32-bit offsets of a tile's rows; grids
+
+extern "C" int64_t laps_fp8_columns(int64_t k) { return k >= 1 && k <= FP8_MAX_K ? fp8_columns(k) : 0; }
+extern "C" int64_t laps_fp8_scale_pitch(int64_t rows) { return rows >= 1 && rows <= FP8_MAX_ROWS ? fp8_pitch(rows) : 0; }
+
+static int fp8_check(const char* who, const laps_ctx* c, const void* x, int rows, int k, const void* codes, const void* scales) {
+    if (!c || !x || !codes || !scales || rows < 1 || rows > FP8_MAX_ROWS || k < 1 || k > FP8_MAX_K) {
+        laps_set_error("%s: NULL pointer or unsupported shape (rows=%d k=%d)", who, rows, k);
+        return LAPS_EINVAL;
+    }
+    if ((((uintptr_t)codes | (uintptr_t)scales) & 15) || ((uintptr_t)x & 1)) {
+        laps_set_error("%s: codes and scales must be 16-byte aligned", who);
+        return LAPS_EINVAL;
+    }
+    return check_current_device(c, who);
+}
+
+extern "C" int laps_fp8_quant(laps_ctx* c, const void* x, int32_t rows, int32_t k, void* codes, void* scales, void* stream) {
+    LAPS_TRY(fp8_check("fp8_quant", c, x, rows, k, codes, scales));
+    return laps_launch_fp8_quant(static_cast<const bf16_t*>(x), rows, k, static_cast<unsigned char*>(codes), static_cast<unsigned char*>(scales),
+                                 static_cast<hipStream_t>(stream));
+}
+
+extern "C" int laps_fp8_dequant(laps_ctx* c, const void* codes, const void* scales, int32_t rows, int32_t k, void* x, void* stream) {
+    LAPS_TRY(fp8_check("fp8_dequant", c, x, rows, k, codes, scales));
+    return laps_launch_fp8_dequant(static_cast<const unsigned char*>(codes), static_cast<const unsigned char*>(scales), rows, k,
+                                   static_cast<bf16_t*>(x), static_cast<hipStream_t>(stream));
+}
+
+static bool fp8_shape(int m, int n, int k) {
+    return m >= 1 && m <= FP8_MAX_ROWS && n >= 1 && n <= FP8_MAX_ROWS && k >= 1 && k <= FP8_MAX_K &&
+           ((long)m + 255) / 256 * (((long)n + 255) / 256) <= (1L << 24);
+}
+
+static size_t fp8_partial_bytes(int m, int n, int k) {
+    const Fp8Plan p = laps_fp8_plan(m, n, (int)fp8_columns(k));
+    return p.split > 1 ? align256((size_t)p.split * m * n * sizeof(float)) : 0;
+}
+
+extern "C" int laps_gemm_fp8_plan_info(int32_t m, int32_t n, int32_t k, int32_t* out) {
+    if (!out || !fp8_shape(m, n, k)) {
+        laps_set_error("gemm_fp8_plan_info: NULL output or unsupported shape (m=%d n=%d k=%d)", m, n, k);
+        return LAPS_EINVAL;
+    }
+    const Fp8Plan p = laps_fp8_plan(m, n, (int)fp8_columns(k));
+    laps_fp8_tile_dims(p.cfg, &out[0], &out[1]);
+    out[2] = p.split;
+    out[3] = p.per * FP8_BLOCK;
+    out[4] = (m + out[0] - 1) / out[0] * ((n + out[1] - 1) / out[1]) * p.split;
+    return LAPS_OK;
+}
+
+extern "C" size_t laps_gemm_fp8_workspace_bytes(int32_t m, int32_t n, int32_t k) { return fp8_shape(m, n, k) ? fp8_partial_bytes(m, n, k) : 0; }
+
+extern "C" int laps_gemm_fp8(laps_ctx* c, const void* a, const void* a_scales, const void* w, const void* w_scales, void* out, int32_t m,
+                             int32_t n, int32_t k, void* ws, size_t ws_bytes, void* stream) {
+    if (!c || !a || !a_scales || !w || !w_scales || !out || !fp8_shape(m, n, k)) {
+        laps_set_error("gemm_fp8: NULL pointer or unsupported shape (m=%d n=%d k=%d)", m, n, k);
+        return LAPS_EINVAL;
+    }
+    if ((((uintptr_t)a | (uintptr_t)a_scales | (uintptr_t)w | (uintptr_t)w_scales) & 15) || ((uintptr_t)out & 1)) {
+        laps_set_error("gemm_fp8: codes and scales must be 16-byte aligned");
+        return LAPS_EINVAL;
+    }
+    LAPS_TRY(check_current_device(c, "gemm_fp8"));
+    const size_t need = fp8_partial_bytes(m, n, k);
+    if (need > 0 && (!ws || ws_bytes < need || ((uintptr_t)ws & 255))) {
+        laps_set_error("gemm_fp8: this shape splits K and needs %zu bytes of 256-byte aligned workspace", need);
+        return LAPS_ENOMEM;
+    }
+    const int columns = (int)fp8_columns(k);
+    return laps_launch_gemm_fp8(laps_fp8_plan(m, n, columns), static_cast<const unsigned char*>(a), static_cast<const unsigned char*>(a_scales),
+                                static_cast<const unsigned char*>(w), static_cast<const unsigned char*>(w_scales), static_cast<bf16_t*>(out), m, n,
+                                columns, static_cast<float*>(ws), static_cast<hipStream_t>(stream));
+}
+
+// Workspace of a projection of bf16 rows: their codes and scales, then the product's.
+static void linear_layout(int m, int n, int k, size_t* scales, size_t* partial, size_t* total) {
+    *scales = align256((size_t)m * fp8_columns(k));
+    *partial = *scales + align256((size_t)(fp8_columns(k) / FP8_BLOCK) * fp8_pitch(m));
+    *total = *partial + fp8_partial_bytes(m, n, k);
+}
+
+extern "C" size_t laps_linear_fp8_workspace_bytes(int32_t m, int32_t n, int32_t k) {
+    if (!fp8_shape(m, n, k)) return 0;
+    size_t scales, partial, total;
+    linear_layout(m, n, k, &scales, &partial, &total);
+    return total;
+}
+
+extern "C" int laps_linear_fp8(laps_ctx* c, const void* x, const void* w, const void* w_scales, void* out, int32_t m, int32_t n, int32_t k,
+                               void* ws, size_t ws_bytes, void* stream) {
+    if (!c || !x || !w || !w_scales || !out || !ws || ((uintptr_t)ws & 255) || !fp8_shape(m, n, k)) {
+        laps_set_error("linear_fp8: NULL pointer, unaligned workspace or unsupported shape (m=%d n=%d k=%d)", m, n, k);
+        return LAPS_EINVAL;
+    }
+    size_t scales, partial, total;
+    linear_layout(m, n, k, &scales, &partial, &total);
+    if (ws_bytes < total) {
+        laps_set_error("linear_fp8: workspace too small (%zu < %zu bytes)", ws_bytes, total);
+        return LAPS_ENOMEM;
+    }
+    unsigned char* w8 = static_cast<unsigned char*>(ws);
+    LAPS_TRY(laps_fp8_quant(c, x, m, k, w8, w8 + scales, stream));
+    return laps_gemm_fp8(c, w8, w8 + scales, w, w_scales, out, m, n, k, w8 + partial, ws_bytes - partial, stream);
 }
 
 extern "C" size_t laps_gemm_workspace_bytes(int32_t m, int32_t n, int32_t k, int32_t split_k) {

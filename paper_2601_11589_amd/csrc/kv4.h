@@ -5,9 +5,6 @@
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 
-constexpr int LAPS_KV4_MAX_PAGES = 1 << 26;       // of a page table's row: positions stay below 2^30
-constexpr long LAPS_KV4_MAX_SEQ_HEADS = 1 << 20;   // sequences times query heads of an attention: its grid
-
 constexpr int KV4_GROUP = 32;   // values of one token and kv head under one scale
 // Bytes of a page of one kv head: the codes of 16 tokens, then their scales (K [token][group], V [group][token]).
 __host__ __device__ constexpr int kv4_codes(int hd) { return LAPS_PAGE * hd / 2; }
@@ -59,24 +56,3 @@ static __device__ __forceinline__ unsigned kv4_codes_of(u32x4 x, int byte) {
 int laps_launch_kv4_move(bool scatter, int n_seq, int n_tokens, const int* cu, const int* start_pos, const int* page_table,
                          int max_pages, void* k_tok, void* v_tok, void* k_pool, void* v_pool, int n_kv, int hd, int n_pool_pages,
                          hipStream_t s);
-
-// attention over 4-bit pools
-struct Kv4Attn {
-    const bf16_t* q;
-    bf16_t* out;
-    const unsigned char *k_pool, *v_pool;
-    const int *cu, *seq_len, *prefix_len, *page_table;   // seq_len may be NULL
-    int n_seq, n_tokens, max_pages, n_pool_pages, n_q, n_kv, hd;
-};
-// Launch of the kernel for few query rows a sequence.
-struct Kv4RowsPlan {
-    int row_tiles;    // 16-row tiles of a block
-    int row_blocks;   // blocks of rows that workgroups of their own walk, a sequence and kv head
-    int parts;        // most parts of a sequence's keys
-    int min_parts;    // as many at least, where there are keys for them
-};
-// Which of the two kernels a launch shape takes: this one, or the blocks of 128 or 256 rows of the bf16 pools' attention.
-bool laps_kv4_takes_rows(int n_seq, int n_tokens, int n_q, int n_kv);
-Kv4RowsPlan laps_kv4_rows_plan(int n_seq, int n_tokens, int n_q, int n_kv, int max_pages);
-size_t laps_kv4_rows_bytes(const Kv4RowsPlan& p, int n_tokens, int n_q, int hd);   // partial results of the parts
-int laps_launch_kv4_rows(const Kv4Attn& a, const Kv4RowsPlan& p, float* partial, hipStream_t s);
