@@ -397,7 +397,7 @@ int laps_attention_kv8(laps_ctx* ctx, int32_t n_seq, int32_t n_tokens, const int
  * matrix instructions add the products of eight k at a time, each cut below 2^-13 of the largest of the eight: 1.5e-5 to 3e-5 of a
  * result in the mean, where bf16 rounds at 2^-9.  Any m, n and k; out needs the alignment of its elements.  A NaN code makes the rows or
  * columns NaN that it belongs to.  workspace_dev: laps_gemm_fp8_workspace_bytes(m, n, k) bytes, 256-byte aligned, for this call alone until
- * its work is done; NULL if that is 0.  EINVAL on NULL, unsupported shapes (as laps_fp8_quant; more than 2^24 tiles of 256 x 256), codes or scales
+ * its work is done; NULL if that is 0.  EINVAL on NULL, unsupported shapes (as laps_fp8_quant; scales of 2^31 bytes; more than 2^22 tiles of 256 x 256), codes or scales
  * that are not 16-byte aligned, or if the context's device is not current; ENOMEM if the workspace is too small. */
 size_t laps_gemm_fp8_workspace_bytes(int32_t m, int32_t n, int32_t k);
 int laps_gemm_fp8(laps_ctx* ctx, const void* a_dev, const void* a_scales_dev, const void* w_dev, const void* w_scales_dev, void* out_dev,

@@ -829,8 +829,9 @@ extern "C" int laps_fp8_dequant(laps_ctx* c, const void* codes, const void* scal
 }
 
 static bool fp8_shape(int m, int n, int k) {
-    return m >= 1 && m <= FP8_MAX_ROWS && n >= 1 && n <= FP8_MAX_ROWS && k >= 1 && k <= FP8_MAX_K &&
-           ((long)m + 255) / 256 * (((long)n + 255) / 256) <= (1L << 24);
+    if (m < 1 || m > FP8_MAX_ROWS || n < 1 || n > FP8_MAX_ROWS || k < 1 || k > FP8_MAX_K) return false;
+    const long blocks = fp8_columns(k) / FP8_BLOCK;   // scales within 32-bit offsets, tiles within the grid's arithmetic
+    return blocks * fp8_pitch(m) < (1L << 31) && blocks * fp8_pitch(n) < (1L << 31) && ((long)m + 255) / 256 * (((long)n + 255) / 256) <= (1L << 22);
 }
 
 static size_t fp8_partial_bytes(int m, int n, int k) {

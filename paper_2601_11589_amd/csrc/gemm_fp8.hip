@@ -3,114 +3,430 @@
 //   C[m, n] = sum over blocks b of 2^(ea[m, b] + ew[n, b]) * sum over the block's 128 k of a[m, k] w[n, k]      in float32, rounded to bf16
 //
 // v_mfma_scale_f32_16x16x128_f8f6f4 takes 128 k of 16 rows of either operand, a whole block, and a scale byte for each row, so the scales
-// cost no instruction of their own.
+// cost no instruction of their own but the reads that bring them.
+//
+// A workgroup of 4 waves owns a BM x BN tile and a slice of K, and walks it in slabs of 128 k: rows of 128 bytes, which go straight into
+// LDS (buffer_load ... lds: no staging registers), the 16-byte chunks XOR-swizzled by the row so that no bank conflicts arise.  Slabs go in
+// half slabs - the rows that one half of every wave's tile needs of A, and one half of W - through a ring of NS of them.  All fragments
+// of a half slab are in registers before its products begin, so a place is free again half a slab after it was waited for; one
+// barrier per half slab waits for the one that is needed next, never for all loads in flight.  Scale bytes lie [block][row], so those of
+// a tile are a few hundred bytes side by side for each slab; each wave fetches one slab's of the next four.
 #include <algorithm>
+#include <type_traits>
 
 #include "fp8.h"
 
 namespace {
 
 typedef __attribute__((ext_vector_type(8))) int i32x8;
+typedef __attribute__((ext_vector_type(4))) int i32x4;
+typedef f32x4 f32x4_a4 __attribute__((aligned(4)));   // the caller's rows are aligned to their elements only
+typedef u32x4 u32x4_a2 __attribute__((aligned(2)));
 
 constexpr int CHUNKS = FP8_BLOCK / 16;   // 16-byte chunks of a row of a slab
+constexpr int NUM_XCD = 8;
+constexpr int GROUP_M = 8;
 
 struct Fp8Args {
     const unsigned char *A, *As, *W, *Ws;   // codes and scale bytes
-    long a_pitch, w_pitch;                  // rows of the scales
+    int a_pitch, w_pitch;                   // rows of the scales
     int M, N, K, split, per, tiles_m, tiles_n;
     bf16_t* out;
     float* partial;                         // [split][M][N] where split > 1
 };
 
-__global__ __launch_bounds__(256, 2) void gemm_fp8_kernel(const Fp8Args g) {
-    constexpr int BM = 128, BN = 128;
-    __shared__ __align__(16) u32x4 sa[BM * CHUNKS], sw[BN * CHUNKS];
-    const int tm = blockIdx.x % g.tiles_m, rest = blockIdx.x / g.tiles_m, tn = rest % g.tiles_n, ks = rest / g.tiles_n;
-    const int m0 = tm * BM, n0 = tn * BN, blocks = g.K / FP8_BLOCK;
-    const int b0 = ks * g.per, b1 = b0 + g.per < blocks ? b0 + g.per : blocks;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave / 2, wn = wave % 2, i = lane & 15, q = lane >> 4;
-    f32x4 acc[4][4];
-#pragma unroll
-    for (int x = 0; x < 4; ++x)
-#pragma unroll
-        for (int y = 0; y < 4; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
-    auto row_of = [](int r, int rows) { return (size_t)(r < rows ? r : rows - 1); };   // rows past the last one are not stored
-    auto swz = [](int row, int chunk) { return row * CHUNKS + (chunk ^ (row & 7)); };
-    for (int b = b0; b < b1; ++b) {
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < BM * CHUNKS / 256; ++j) {
-            const int row = (tid + 256 * j) / CHUNKS, c = tid % CHUNKS;
-            sa[swz(row, c)] = *reinterpret_cast<const u32x4*>(g.A + row_of(m0 + row, g.M) * g.K + (size_t)b * FP8_BLOCK + c * 16);
-            sw[swz(row, c)] = *reinterpret_cast<const u32x4*>(g.W + row_of(n0 + row, g.N) * g.K + (size_t)b * FP8_BLOCK + c * 16);
-        }
-        __syncthreads();
-        i32x8 fa[4], fw[4];
-        int ea[4], ew[4];
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            // which 32 of the 128 k a lane holds does not matter, as long as both operands agree
-            const int ra = wm * 64 + x * 16 + i, rw = wn * 64 + x * 16 + i;
-            auto two = [](u32x4 lo, u32x4 hi) {
-                return i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
-            };
-            fa[x] = two(sa[swz(ra, q)], sa[swz(ra, q + 4)]);
-            fw[x] = two(sw[swz(rw, q)], sw[swz(rw, q + 4)]);
-            ea[x] = g.As[b * g.a_pitch + row_of(m0 + ra, g.M)];
-            ew[x] = g.Ws[b * g.w_pitch + row_of(n0 + rw, g.N)];
-        }
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-#pragma unroll
-            for (int y = 0; y < 4; ++y)
-                acc[x][y] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[y], fa[x], acc[x][y], 0, 0, 0, ew[y], 0, ea[x]);
+// x / d of a uniform x >= 0, off by one at most below 2^23 before the correction.
+__device__ __forceinline__ int fast_div(int x, int d) {
+    const int q = (int)((float)x * __builtin_amdgcn_rcpf((float)d));
+    const int r = x - q * d;
+    return __builtin_amdgcn_readfirstlane(q + (r >= d ? 1 : 0) - (r < 0 ? 1 : 0));
+}
+
+// Workgroup -> (row tile, column tile, K slice): each of the 8 XCDs, to which workgroups are dealt in turn, gets a contiguous range of
+// tiles, walked M-fastest in groups of 8 row tiles, so that the workgroups that share a weight panel share an L2.
+struct Tile { int tm, tn, ks; };
+__device__ __forceinline__ Tile tile_of(int bid, const Fp8Args& g) {
+    const int total = g.tiles_m * g.tiles_n * g.split, q = total / NUM_XCD, r = total % NUM_XCD, xcd = bid % NUM_XCD;
+    const int lin = xcd * q + (xcd < r ? xcd : r) + bid / NUM_XCD, slice = g.tiles_m * g.tiles_n;
+    Tile c;
+    c.ks = g.split == 1 ? 0 : fast_div(lin, slice);
+    const int t = lin - c.ks * slice;
+    if (g.tiles_m == 1) {
+        c.tm = 0;
+        c.tn = t;
+        return c;
     }
-    // a lane holds columns 4 q .. 4 q + 3 of row i of a sub-tile
+    const int size = GROUP_M * g.tiles_n, grp = fast_div(t, size), first = grp * GROUP_M;
+    const int gm = g.tiles_m - first < GROUP_M ? g.tiles_m - first : GROUP_M, in = t - grp * size;
+    c.tn = fast_div(in, gm);
+    c.tm = first + in - c.tn * gm;
+    return c;
+}
+
+template <int BM, int BN, int WM, int WN>
+struct Shape {
+    static constexpr int WTM = BM / WM, WTN = BN / WN;                   // wave tile
+    static constexpr int MI = WTM / 16, NI = WTN / 16;
+    static constexpr int HA = BM / 2, HB = BN / 2;                       // rows of a half slab
+    static constexpr int QA = HA / 4, QB = HB / 4;                       // rows that one wave loads
+    static constexpr int LA = QA / 8, LB = QB / 8;                       // load instructions of a wave: 8 rows of 128 bytes
+    static constexpr int LOADS = LA + LB;
+    static constexpr int SLOT = (HA + HB) * FP8_BLOCK;                   // bytes
+    static constexpr bool TWO = BM * BN <= 128 * 128;                    // two workgroups on a compute unit
+    static constexpr int SCALES = 2 * 4 * 512;                           // two groups of four slabs: 256 rows of A, 256 of W
+    static constexpr int CAP = (TWO ? 80 : 160) * 1024 - SCALES;
+    static constexpr int NS = CAP / SLOT < 6 ? CAP / SLOT : 6;           // half slabs in LDS
+    static constexpr int LDS = SCALES + NS * SLOT;
+    static_assert(WM * WN == 4 && QA % 8 == 0 && QB % 8 == 0 && NS >= 3, "four waves load whole groups of rows");
+    static_assert((WTM / 2) % 16 == 0 && (WTN / 2) % 32 == 0, "halves of whole sub-tiles, pairs of columns");
+    static_assert((WTM / 2) % QA == 0 && (WTN / 2) % QB == 0, "the rows that a wave loads lie in one wave tile");
+};
+
+// LDS rows are 128 bytes; chunk c of row r is stored at chunk position c ^ key: the 16 rows of a fragment have, two by two, 8 different
+// keys.  Fragment row i of sub-tile s is row 16 s + i of A, and row 32 (s / 2) + 8 (i / 4) + 4 (s % 2) + i % 4 of W: a lane, which
+// holds columns 4 q .. 4 q + 3 of a sub-tile of the product, then has eight neighbouring columns in two of them.
+__device__ __forceinline__ int key_a(int row) { return (row >> 1) & 7; }
+__device__ __forceinline__ int key_w(int row) { return ((row >> 1) & 1) | (((row >> 3) & 3) << 1); }
+
+// The matrix instructions are inline assembly: the builtin has separate accumulator operands in and out, and the register allocator
+// fills the loop with moves between them.  The compiler therefore does not know the wait states between them and what else touches
+// their accumulators; every accumulator passes through a statement behind the wait.
+template <typename S>
+__device__ __forceinline__ void acc_fence(f32x4 (&acc)[S::MI][S::NI]) {
+    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-        const int m = m0 + wm * 64 + x * 16 + i;
+    for (int mi = 0; mi < S::MI; ++mi)
+#pragma unroll
+        for (int ni = 0; ni < S::NI; ++ni) {
+            if (S::TWO) asm volatile("" : "+v"(acc[mi][ni]));
+            else asm volatile("" : "+a"(acc[mi][ni]));
+        }
+}
+
+template <int V>
+constexpr std::integral_constant<int, V> I{};
+
+// all but the last N loads of this wave have landed and its LDS reads are done; so are the other waves'
+template <int N>
+__device__ __forceinline__ void dma_barrier() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// Stores of a tile.  GUARD: it reaches past column N.
+template <typename S, bool PARTIAL, bool GUARD>
+__device__ __forceinline__ void store_tile(const f32x4 (&acc)[S::MI][S::NI], const Fp8Args& g, int ks, int row0, int col0) {
+    // a lane holds columns 8 q .. 8 q + 7 of the 32 that two sub-tiles make; col0 counts them in
+#pragma unroll
+    for (int mi = 0; mi < S::MI; ++mi) {
+        const int m = row0 + mi * 16;
         if (m >= g.M) continue;
 #pragma unroll
-        for (int y = 0; y < 4; ++y)
+        for (int j = 0; j < S::NI / 2; ++j) {
+            const int n = col0 + 32 * j;
+            const f32x4 lo = acc[mi][2 * j], hi = acc[mi][2 * j + 1];
+            if constexpr (PARTIAL) {
+                float* to = g.partial + ((size_t)ks * g.M + m) * g.N + n;
+                if (!GUARD || n + 8 <= g.N) {
+                    reinterpret_cast<f32x4_a4*>(to)[0] = lo;
+                    reinterpret_cast<f32x4_a4*>(to)[1] = hi;
+                } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int n = n0 + wn * 64 + y * 16 + 4 * q + e;
-                if (n >= g.N) continue;
-                if (g.split == 1) g.out[(size_t)m * g.N + n] = f32_to_bf16(acc[x][y][e]);
-                else g.partial[((size_t)ks * g.M + m) * g.N + n] = acc[x][y][e];
+                    for (int e = 0; e < 8; ++e)
+                        if (n + e < g.N) to[e] = e < 4 ? lo[e % 4] : hi[e % 4];
+                }
+            } else {
+                bf16_t* to = g.out + (size_t)m * g.N + n;
+                if (!GUARD || n + 8 <= g.N) {
+                    *reinterpret_cast<u32x4_a2*>(to) = u32x4{pack_bf16x2(lo.x, lo.y), pack_bf16x2(lo.z, lo.w), pack_bf16x2(hi.x, hi.y), pack_bf16x2(hi.z, hi.w)};
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (n + e < g.N) to[e] = f32_to_bf16(e < 4 ? lo[e % 4] : hi[e % 4]);
+                }
             }
+        }
     }
 }
 
-// The slices' sums, in order.
-__global__ __launch_bounds__(256) void fp8_sum_kernel(const float* __restrict__ partial, int split, long count, bf16_t* __restrict__ out) {
-    const long i = (long)blockIdx.x * 256 + threadIdx.x;
-    if (i >= count) return;
-    float sum = partial[i];
-    for (int s = 1; s < split; ++s) sum += partial[s * count + i];
-    out[i] = f32_to_bf16(sum);
+// STREAM: nobody else reads this tile's weights (a single row tile), they bypass the caches.
+template <int BM, int BN, int WM, int WN, bool PARTIAL, bool STREAM>
+__device__ __forceinline__ void gemm_tile(const Fp8Args& g, unsigned char* smem) {
+    using S = Shape<BM, BN, WM, WN>;
+    constexpr int MH = S::MI / 2, NH = S::NI / 2, NS = S::NS;
+    const int K = g.K;
+    const Tile tc = tile_of(blockIdx.x, g);
+    const int m0 = tc.tm * BM, n0 = tc.tn * BN, blocks = K / FP8_BLOCK;
+    const int b0 = tc.ks * g.per, KT = b0 + g.per < blocks ? g.per : blocks - b0;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / WN, wn = wave % WN, lrow = lane & 15, lk = lane >> 4;
+
+    auto rsrc = [&](const unsigned char* base, unsigned bytes) {
+        const unsigned long long p = reinterpret_cast<unsigned long long>(base);
+        return i32x4{__builtin_amdgcn_readfirstlane((int)(unsigned)p), __builtin_amdgcn_readfirstlane((int)(p >> 32)),
+                     __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000};
+    };
+    // Rows past the last one lie behind their descriptor's end: no request is made for them, and zeros arrive.
+    const int rows_a = g.M - m0 < BM ? g.M - m0 : BM, rows_w = g.N - n0 < BN ? g.N - n0 : BN;
+    i32x4 ra = rsrc(g.A + (size_t)m0 * K, (unsigned)rows_a * (unsigned)K), rb = rsrc(g.W + (size_t)n0 * K, (unsigned)rows_w * (unsigned)K);
+    const int a_bytes = ra[2], b_bytes = rb[2];
+    // scales of this slice's blocks from the tile's first row on, cut to the array's end
+    auto scale_rsrc = [&](const unsigned char* base, int pitch, int first) {
+        const size_t at = (size_t)b0 * pitch + first, end = (size_t)blocks * pitch, left = end - at;
+        return rsrc(base + at, (unsigned)(left < 0x7fffffffu ? left : 0x7fffffffu));
+    };
+    const i32x4 rsa = scale_rsrc(g.As, g.a_pitch, m0), rsb = scale_rsrc(g.Ws, g.w_pitch, n0);
+    // offsets of a lane's chunks: half slab row x -> tile row (x / (WT / 2)) * WT + half * WT / 2 + x % (WT / 2)
+    unsigned va[2][S::LA], vb[2][S::LB];
+    {
+        const int qa = wave * S::QA, qb = wave * S::QB;
+        const int ta = qa / (S::WTM / 2) * S::WTM + qa % (S::WTM / 2), tb = qb / (S::WTN / 2) * S::WTN + qb % (S::WTN / 2);
+        const int r = lane >> 3, c = lane & 7;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int i = 0; i < S::LA; ++i)
+                va[h][i] = (unsigned)(ta + h * S::WTM / 2 + 8 * i + r) * (unsigned)K + (c ^ key_a(qa + 8 * i + r)) * 16 + (unsigned)b0 * FP8_BLOCK;
+#pragma unroll
+            for (int i = 0; i < S::LB; ++i)
+                vb[h][i] = (unsigned)(tb + h * S::WTN / 2 + 8 * i + r) * (unsigned)K + (c ^ key_w(qb + 8 * i + r)) * 16 + (unsigned)b0 * FP8_BLOCK;
+        }
+    }
+    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
+    const unsigned lds_a = lds0 + S::SCALES + wave * S::QA * 128, lds_b = lds0 + S::SCALES + S::HA * 128 + wave * S::QB * 128;
+    // load i of a half slab (A rows ha, W rows hb) into the slot at byte `slot`
+    auto dma = [&](int i, int ha, int hb, unsigned slot, int koff) {
+        if (i < S::LA) {
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                         ::"s"(lds_a + slot + i * 1024), "v"(va[ha][i]), "s"(ra), "s"(koff));
+            return;
+        }
+        const int j = i - S::LA;
+        if (STREAM)
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen nt lds"
+                         ::"s"(lds_b + slot + j * 1024), "v"(vb[hb][j]), "s"(rb), "s"(koff));
+        else
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                         ::"s"(lds_b + slot + j * 1024), "v"(vb[hb][j]), "s"(rb), "s"(koff));
+    };
+    // this wave's slab of scales among the four from `first` on: 256 rows of A and of W, four a lane; slabs past the last one bring bytes
+    // that nothing uses
+    auto scale_dma = [&](int first) {
+        const int kt = first + wave;
+        const unsigned to = lds0 + (unsigned)(first >> 2 & 1) * 2048u + wave * 512u;
+        // in the lane's offset, which the descriptor's bound sees: the last block's may reach past the array
+        const unsigned at_a = (unsigned)kt * (unsigned)g.a_pitch + lane * 4, at_w = (unsigned)kt * (unsigned)g.w_pitch + lane * 4;
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(at_a), "s"(rsa));
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to + 256u), "v"(at_w), "s"(rsb));
+    };
+
+    f32x4 acc[S::MI][S::NI];
+#pragma unroll
+    for (int mi = 0; mi < S::MI; ++mi)
+#pragma unroll
+        for (int ni = 0; ni < S::NI; ++ni) acc[mi][ni] = f32x4{0.f, 0.f, 0.f, 0.f};
+    i32x8 fa[S::MI], fb[S::NI];
+    int ea[S::MI], eb[S::NI];
+    const u32x4* L = reinterpret_cast<const u32x4*>(smem + S::SCALES);
+    const int key = (lrow >> 1) & 7, w_row = 8 * (lrow >> 2) + (lrow & 3);   // both keys of fragment row lrow are this one
+    const int src_a = (wm * (S::WTM / 2) + lrow) * CHUNKS, src_b = (S::HA + wn * (S::WTN / 2) + w_row) * CHUNKS;
+    const unsigned char *scale_a = smem + wm * S::WTM + lrow, *scale_b = smem + 256 + wn * S::WTN + w_row;
+    auto scale_at = [](int kt) { return (kt >> 2 & 1) * 2048 + (kt & 3) * 512; };
+    auto put = [](i32x8& f, int half, u32x4 x) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[4 * half + e] = (int)x[e];
+    };
+    // read i of half h of A (W): 2 MH (2 NH) chunks, then the scales.  Which 32 of a block's k a lane holds does not matter, as long as both
+    // operands agree: chunks lk and lk + 4.
+    auto read_a = [&](int h, int i, unsigned slot, int kt) {
+        if (i < 2 * MH) put(fa[h * MH + i / 2], i & 1, L[slot / 16 + src_a + i / 2 * 16 * CHUNKS + ((lk + (i & 1) * 4) ^ key)]);
+        else ea[h * MH + i - 2 * MH] = scale_a[scale_at(kt) + h * (S::WTM / 2) + (i - 2 * MH) * 16];
+    };
+    auto read_b = [&](int h, int i, unsigned slot, int kt) {
+        const int ni = i < 2 * NH ? i / 2 : i - 2 * NH, row = ni / 2 * 32 + ni % 2 * 4;
+        if (i < 2 * NH) put(fb[h * NH + ni], i & 1, L[slot / 16 + src_b + row * CHUNKS + ((lk + (i & 1) * 4) ^ key)]);
+        else eb[h * NH + ni] = scale_b[scale_at(kt) + h * (S::WTN / 2) + row];
+    };
+
+    // Products of a slab: four quadrants of the wave's tile, each with one new half of A or W:
+    //   even slabs   A0W0 | read W1,  A0W1 | read A1,  A1W1 | read the next slab's A0,  A1W0 | read its W1
+    //   odd slabs    A0W1 | read W0,  A0W0 | read A1,  A1W0 | read the next slab's A0,  A1W1 | read its W0
+    // Half slab p is what quadrants 2p - 2 and 2p - 1 read: A half p % 2 and W half (p ^ (p >> 1)) & 1 of slab p / 2.  While
+    // half slab p is multiplied, p + 1 is read and p + NS is loaded into the place of p.
+    // Slabs past the last one are loaded from descriptors of no bytes, which takes no request.
+    auto until = [&](int k) {
+        ra[2] = k < KT ? a_bytes : 0;
+        rb[2] = k < KT ? b_bytes : 0;
+        return (k < KT ? k : KT - 1) * FP8_BLOCK;
+    };
+    scale_dma(0);
+#pragma unroll
+    for (int p = 0; p < NS; ++p) {
+        const int koff = until(p / 2);
+#pragma unroll
+        for (int i = 0; i < S::LOADS; ++i) dma(i, p & 1, (p ^ (p >> 1)) & 1, p * S::SLOT, koff);
+    }
+    dma_barrier<(NS - 1) * S::LOADS>();
+#pragma unroll
+    for (int i = 0; i < 3 * MH; ++i) read_a(0, i, 0, 0);
+#pragma unroll
+    for (int i = 0; i < 3 * NH; ++i) read_b(0, i, 0, 0);
+    acc_fence<S>(acc);
+    dma_barrier<(NS - 2) * S::LOADS>();
+
+    unsigned rd = S::SLOT, wr = 0;   // places of half slabs p + 1 and p
+    // One quadrant: rows half ma times columns half nb.  Spread over the first three quarters of its matrix instructions, so that the
+    // barrier finds the reads done: the fragments of half rh of A or W of slab kt, and loads [l0, l1) of half slab p + NS.
+    auto quadrant = [&](auto ma, auto nb, auto rd_a, auto rh, int kt, auto l0, auto l1, auto ha, auto hb, int koff) {
+        constexpr int NM = MH * NH, SPAN = (NM * 3 + 3) / 4;
+        constexpr int NR = rd_a() ? 3 * MH : 3 * NH, NL = l1() - l0(), OPS = NR + NL;
+#pragma unroll
+        for (int i = 0; i < NM; ++i) {
+            const int nr = i / MH, mi = ma() * MH + (nr & 1 ? MH - 1 - i % MH : i % MH), ni = nb() * NH + nr;
+            if (S::TWO)
+                asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0]"
+                             : "+v"(acc[mi][ni]) : "v"(fb[ni]), "v"(fa[mi]), "v"(eb[ni]), "v"(ea[mi]));
+            else
+                asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0]"
+                             : "+a"(acc[mi][ni]) : "v"(fb[ni]), "v"(fa[mi]), "v"(eb[ni]), "v"(ea[mi]));
+            const int j0 = i < SPAN ? i * OPS / SPAN : OPS, j1 = i + 1 < SPAN ? (i + 1) * OPS / SPAN : OPS;
+#pragma unroll
+            for (int j = j0; j < j1; ++j) {
+                const int nl = j * NL / OPS;   // loads among the operations before j
+                if ((j + 1) * NL / OPS > nl) dma(l0() + nl, ha(), hb(), wr, koff);
+                else if (rd_a()) read_a(rh(), j - nl, rd, kt);
+                else read_b(rh(), j - nl, rd, kt);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    auto half_end = [&]() {
+        dma_barrier<(NS - 2) * S::LOADS>();
+        __builtin_amdgcn_sched_barrier(0);
+        wr = rd;
+        rd = rd + S::SLOT == NS * S::SLOT ? 0u : rd + S::SLOT;
+        asm volatile("" : "+s"(rd), "+s"(wr));   // one address per operand, not one for every place of the ring
+    };
+    auto slab = [&](auto parity, int kt) {
+        constexpr int B = decltype(parity)::value;   // the columns half this slab begins with
+        constexpr int P0 = 2 * B, P1 = 2 * B + 1;    // p modulo 4
+        constexpr int N0 = (P0 + NS) & 3, N1 = (P1 + NS) & 3, H0 = (N0 ^ (N0 >> 1)) & 1, H1 = (N1 ^ (N1 >> 1)) & 1;
+        constexpr int LH = S::LOADS / 2;
+        // scales: four slabs ahead of their first use at the least, three and a half behind the last one of those they replace
+        if (B == 0 && (kt & 3) == 0 && kt + 4 < KT) scale_dma(kt + 4);
+        const int o0 = until(kt + NS / 2);           // half slab p + NS lies in slab (p + NS) / 2
+        quadrant(I<0>, I<B>, I<0>, I<B ^ 1>, kt, I<0>, I<LH>, I<(N0 & 1)>, I<H0>, o0);
+        quadrant(I<0>, I<B ^ 1>, I<1>, I<1>, kt, I<LH>, I<S::LOADS>, I<(N0 & 1)>, I<H0>, o0);
+        half_end();
+        const int o1 = until(kt + (1 + NS) / 2);
+        quadrant(I<1>, I<B ^ 1>, I<1>, I<0>, kt + 1, I<0>, I<LH>, I<(N1 & 1)>, I<H1>, o1);
+        quadrant(I<1>, I<B>, I<0>, I<B ^ 1>, kt + 1, I<LH>, I<S::LOADS>, I<(N1 & 1)>, I<H1>, o1);
+        half_end();
+    };
+    for (int kt = 0;;) {
+        slab(I<0>, kt);
+        if (++kt >= KT) break;
+        slab(I<1>, kt);
+        if (++kt >= KT) break;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load may land after this workgroup's LDS is another's
+    acc_fence<S>(acc);
+    const int row0 = m0 + wm * S::WTM + lrow, col0 = n0 + wn * S::WTN + 8 * lk;
+    if (__builtin_expect(n0 + BN > g.N, 0)) store_tile<S, PARTIAL, true>(acc, g, tc.ks, row0, col0);
+    else store_tile<S, PARTIAL, false>(acc, g, tc.ks, row0, col0);
 }
+
+template <int BM, int BN, int WM, int WN, bool PARTIAL, bool STREAM>
+__global__ __launch_bounds__(256, (Shape<BM, BN, WM, WN>::TWO ? 2 : 1)) void gemm_fp8_kernel(const Fp8Args g) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    gemm_tile<BM, BN, WM, WN, PARTIAL, STREAM>(g, smem);
+}
+
+// The slices' sums, in order, eight columns of the flattened result a thread.
+__global__ __launch_bounds__(256) void fp8_sum_kernel(const float* __restrict__ partial, int split, long count, bf16_t* __restrict__ out) {
+    const long i = ((long)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (i >= count) return;
+    if (i + 8 <= count) {
+        f32x4 lo = reinterpret_cast<const f32x4_a4*>(partial + i)[0], hi = reinterpret_cast<const f32x4_a4*>(partial + i)[1];
+#pragma unroll 4
+        for (int s = 1; s < split; ++s) {
+            lo += reinterpret_cast<const f32x4_a4*>(partial + s * count + i)[0];
+            hi += reinterpret_cast<const f32x4_a4*>(partial + s * count + i)[1];
+        }
+        *reinterpret_cast<u32x4_a2*>(out + i) = u32x4{pack_bf16x2(lo.x, lo.y), pack_bf16x2(lo.z, lo.w), pack_bf16x2(hi.x, hi.y), pack_bf16x2(hi.z, hi.w)};
+        return;
+    }
+    for (long j = i; j < count; ++j) {
+        float sum = partial[j];
+        for (int s = 1; s < split; ++s) sum += partial[s * count + j];
+        out[j] = f32_to_bf16(sum);
+    }
+}
+
+template <int BM, int BN, int WM, int WN, bool PARTIAL, bool STREAM>
+int launch(const Fp8Args& g, hipStream_t s) {
+    auto kern = gemm_fp8_kernel<BM, BN, WM, WN, PARTIAL, STREAM>;
+    constexpr int lds = Shape<BM, BN, WM, WN>::LDS;
+    static bool attr_set = false;
+    if (!attr_set) {   // per kernel; idempotent, so a race only repeats the call
+        LAPS_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+        attr_set = true;
+    }
+    hipLaunchKernelGGL(kern, dim3(g.tiles_m * g.tiles_n * g.split), dim3(256), lds, s, g);
+    LAPS_LAUNCH_CHECK();
+    return LAPS_OK;
+}
+
+template <int BM, int BN, int WM, int WN>
+int launch_tile(const Fp8Args& g, hipStream_t s) {
+    if (g.tiles_m == 1) return g.split > 1 ? launch<BM, BN, WM, WN, true, true>(g, s) : launch<BM, BN, WM, WN, false, true>(g, s);
+    return g.split > 1 ? launch<BM, BN, WM, WN, true, false>(g, s) : launch<BM, BN, WM, WN, false, false>(g, s);
+}
+
+struct TileDef { int bm, bn; };
+constexpr TileDef kTiles[] = {{64, 128}, {64, 256}, {128, 128}, {128, 256}, {192, 256}, {256, 128}, {256, 192}, {256, 256}};   // index = Fp8Plan::cfg
+constexpr int kNumTiles = sizeof(kTiles) / sizeof(kTiles[0]);
 
 }  // namespace
 
-void laps_fp8_tile_dims(int cfg, int* bm, int* bn) { *bm = *bn = cfg == 0 ? 128 : 0; }
+void laps_fp8_tile_dims(int cfg, int* bm, int* bn) {
+    *bm = cfg >= 0 && cfg < kNumTiles ? kTiles[cfg].bm : 0;
+    *bn = cfg >= 0 && cfg < kNumTiles ? kTiles[cfg].bn : 0;
+}
 
 Fp8Plan laps_fp8_plan(int m, int n, int k) {
     const int blocks = k / FP8_BLOCK;
-    const long tiles = ((m + 127L) / 128) * ((n + 127L) / 128);
+    const int cfg = m <= 64 ? 0 : m <= 128 ? 2 : 7;
+    const long tiles = ((m + (long)kTiles[cfg].bm - 1) / kTiles[cfg].bm) * ((n + (long)kTiles[cfg].bn - 1) / kTiles[cfg].bn);
     long split = std::max(1L, std::min(256 / tiles, (long)blocks / 4));
     const int per = (int)((blocks + split - 1) / split);
-    return {0, (blocks + per - 1) / per, per};
+    return {cfg, (blocks + per - 1) / per, per};
 }
 
 int laps_launch_gemm_fp8(const Fp8Plan& p, const unsigned char* a, const unsigned char* a_scales, const unsigned char* w,
                          const unsigned char* w_scales, bf16_t* out, int m, int n, int k, float* partial, hipStream_t s) {
-    Fp8Args g = {a, a_scales, w, w_scales, fp8_pitch(m), fp8_pitch(n), m, n, k, p.split, p.per, (m + 127) / 128, (n + 127) / 128, out, partial};
-    hipLaunchKernelGGL(gemm_fp8_kernel, dim3((unsigned)((long)g.tiles_m * g.tiles_n * p.split)), dim3(256), 0, s, g);
-    LAPS_LAUNCH_CHECK();
+    int bm, bn;
+    laps_fp8_tile_dims(p.cfg, &bm, &bn);
+    if (bm == 0) {
+        laps_set_error("gemm_fp8: no tile %d", p.cfg);
+        return LAPS_EINVAL;
+    }
+    const Fp8Args g = {a, a_scales, w, w_scales, (int)fp8_pitch(m), (int)fp8_pitch(n), m, n, k, p.split, p.per, (m + bm - 1) / bm, (n + bn - 1) / bn,
+                       out, partial};
+    int rc = LAPS_EINVAL;
+    switch (p.cfg) {
+        case 0: rc = launch_tile<64, 128, 2, 2>(g, s); break;
+        case 1: rc = launch_tile<64, 256, 1, 4>(g, s); break;
+        case 2: rc = launch_tile<128, 128, 2, 2>(g, s); break;
+        case 3: rc = launch_tile<128, 256, 1, 4>(g, s); break;
+        case 4: rc = launch_tile<192, 256, 2, 2>(g, s); break;
+        case 5: rc = launch_tile<256, 128, 2, 2>(g, s); break;
+        case 6: rc = launch_tile<256, 192, 4, 1>(g, s); break;
+        case 7: rc = launch_tile<256, 256, 2, 2>(g, s); break;
+    }
+    LAPS_TRY(rc);
     if (p.split > 1) {
         const long count = (long)m * n;
-        hipLaunchKernelGGL(fp8_sum_kernel, dim3((unsigned)((count + 255) / 256)), dim3(256), 0, s, partial, p.split, count, out);
+        hipLaunchKernelGGL(fp8_sum_kernel, dim3((unsigned)((count + 2047) / 2048)), dim3(256), 0, s, partial, p.split, count, out);
         LAPS_LAUNCH_CHECK();
     }
     return LAPS_OK;

@@ -126,8 +126,8 @@ def test_plans_of_products_hold_what_their_kernels_assume():
 
 
 def test_plans_of_products_refuse():
-    assert product_plan(1, 1, 1) is not None and product_plan(1 << 24, 1, 1 << 22) is not None
-    for bad in ((0, 1, 1), (1, 0, 1), (1, 1, 0), (1, 1, (1 << 22) + 1), ((1 << 24) + 1, 1, 1), (1, (1 << 24) + 1, 1), (1 << 24, 1 << 24, 128), (-1, 5, 5)):
+    assert product_plan(1, 1, 1) is not None and product_plan(1 << 24, 1, 128 * 127) is not None
+    for bad in ((0, 1, 1), (1, 0, 1), (1, 1, 0), (1, 1, (1 << 22) + 1), ((1 << 24) + 1, 1, 1), (1, (1 << 24) + 1, 1), (1 << 24, 1 << 24, 128), (1 << 24, 1, 128 * 128), (1, 1 << 24, 1 << 22), (-1, 5, 5)):
         assert product_plan(*bad) is None and api.lib().laps_gemm_fp8_workspace_bytes(*bad) == 0, bad
         assert api.lib().laps_linear_fp8_workspace_bytes(*bad) == 0, bad
 
