@@ -902,6 +902,16 @@ extern "C" int laps_linear_fp8(laps_ctx* c, const void* x, const void* w, const 
         laps_set_error("linear_fp8: workspace too small (%zu < %zu bytes)", ws_bytes, total);
         return LAPS_ENOMEM;
     }
+    const bf16_t* rows = static_cast<const bf16_t*>(x);
+    if (laps_fp8_takes_bf16_rows(laps_fp8_plan(m, n, (int)fp8_columns(k)), rows, m, k)) {
+        if ((((uintptr_t)w | (uintptr_t)w_scales) & 15) || ((uintptr_t)out & 1)) {
+            laps_set_error("linear_fp8: codes and scales must be 16-byte aligned");
+            return LAPS_EINVAL;
+        }
+        LAPS_TRY(check_current_device(c, "linear_fp8"));
+        return laps_launch_linear_fp8_rows(rows, static_cast<const unsigned char*>(w), static_cast<const unsigned char*>(w_scales),
+                                           static_cast<bf16_t*>(out), m, n, k, static_cast<hipStream_t>(stream));
+    }
     unsigned char* w8 = static_cast<unsigned char*>(ws);
     LAPS_TRY(laps_fp8_quant(c, x, m, k, w8, w8 + scales, stream));
     return laps_gemm_fp8(c, w8, w8 + scales, w, w_scales, out, m, n, k, w8 + partial, ws_bytes - partial, stream);

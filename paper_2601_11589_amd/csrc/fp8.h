@@ -31,6 +31,16 @@ static __device__ __forceinline__ unsigned bf16_amax(u32x4 x) {
     return m.x > m.y ? m.x : m.y;
 }
 
+static __device__ __forceinline__ unsigned bf16_amax_finite(u32x4 x) {   // of the finite ones
+    unsigned top = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const unsigned w = x[j / 2] >> (16 * (j % 2)) & 0x7fffu;
+        top = w < BF16_INF && w > top ? w : top;
+    }
+    return top;
+}
+
 // Codes of eight bf16 values under 2^(byte - 127): to nearest, ties to the even code, what is not finite to NaN.  The conversion makes
 // magnitudes of 464 and more NaN, which a scale below the highest never meets; under that one they are cut to 448 first.
 static __device__ __forceinline__ u32x2 fp8_codes_of(u32x4 x, int byte) {
@@ -90,3 +100,6 @@ void laps_fp8_tile_dims(int cfg, int* bm, int* bn);
 // out bf16 [m][n] = a w^T; partial: split * m * n floats if split > 1.  k is a multiple of 128.
 int laps_launch_gemm_fp8(const Fp8Plan& p, const unsigned char* a, const unsigned char* a_scales, const unsigned char* w,
                          const unsigned char* w_scales, bf16_t* out, int m, int n, int k, float* partial, hipStream_t s);
+// A projection of bf16 rows in one launch, without their codes in memory: whether the plan has one for them, and the launch.
+bool laps_fp8_takes_bf16_rows(const Fp8Plan& p, const bf16_t* x, int m, int k);
+int laps_launch_linear_fp8_rows(const bf16_t* x, const unsigned char* w, const unsigned char* w_scales, bf16_t* out, int m, int n, int k, hipStream_t s);

@@ -43,14 +43,7 @@ __global__ __launch_bounds__(ROWS * 16) void fp8_quant_kernel(const bf16_t* __re
     for (int i = 0; i < BLOCKS; ++i) {
         if (b0 + i >= n) break;
         unsigned top = bf16_amax(v[i]);
-        if (top >= BF16_INF) {   // of the finite ones
-            top = 0;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const unsigned w = v[i][j / 2] >> (16 * (j % 2)) & 0x7fffu;
-                top = w < BF16_INF && w > top ? w : top;
-            }
-        }
+        if (top >= BF16_INF) top = bf16_amax_finite(v[i]);
 #pragma unroll
         for (int s = 1; s < 16; s <<= 1) {
             const unsigned o = __shfl_xor(top, s, 64);

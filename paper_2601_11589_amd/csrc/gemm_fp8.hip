@@ -341,6 +341,100 @@ __global__ __launch_bounds__(256, (Shape<BM, BN, WM, WN>::TWO ? 2 : 1)) void gem
     gemm_tile<BM, BN, WM, WN, PARTIAL, STREAM>(g, smem);
 }
 
+// ------------------------------------------------------------------ up to 16 rows
+// Weights that one launch's latency outweighs.  Nothing is staged: a wave takes 16 columns and up to U blocks of 128 k, 2 KB of weights a block
+// straight into the operand registers of one matrix instruction, all on their way before the first is used; the WAVES waves of a
+// workgroup share the blocks and add up in LDS.  One launch, no partial results.  Lane (i, q) = (lane % 16, lane / 16) holds the 32 k from 32 q
+// on of row i, on both sides.
+// QUANT: the rows are bf16 and become codes on the way, in every workgroup again, which spares the launch that would do it once.
+struct RowsArgs {
+    const unsigned char *a, *a_scales;   // of codes
+    const bf16_t* x;                     // of bf16 rows
+    const unsigned char *w, *w_scales;
+    bf16_t* out;
+    int m, n, k, columns, a_pitch, w_pitch;
+};
+
+template <int WAVES, int U, bool QUANT>
+__device__ __forceinline__ void rows_tile(const RowsArgs& g, f32x4 (*red)[64]) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, q = lane >> 4;
+    const int n0 = blockIdx.x * 16, blocks = g.columns / FP8_BLOCK, mine = (blocks - wave + WAVES - 1) / WAVES;   // wave, wave + WAVES, ...
+    // rows past the last one are the last one again: no request of their own, not stored
+    const size_t row = i < g.m ? i : g.m - 1, col = n0 + i < g.n ? n0 + i : g.n - 1;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    if (mine > 0) {
+        u32x4 w[U][2], a[U][QUANT ? 4 : 2];
+        int ew[U], ea[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int b = wave + (u < mine ? u : mine - 1) * WAVES;   // past the end: the last block again, not used
+            const u32x4* wp = reinterpret_cast<const u32x4*>(g.w + col * g.columns + (size_t)b * FP8_BLOCK + q * 32);
+            w[u][0] = __builtin_nontemporal_load(wp);
+            w[u][1] = __builtin_nontemporal_load(wp + 1);
+            ew[u] = g.w_scales[(size_t)b * g.w_pitch + col];
+            if constexpr (QUANT) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int c = b * FP8_BLOCK + q * 32 + j * 8;
+                    a[u][j] = *reinterpret_cast<const u32x4*>(g.x + row * g.k + (c < g.k ? c : 0));
+                }
+            } else {
+                const u32x4* ap = reinterpret_cast<const u32x4*>(g.a + row * g.columns + (size_t)b * FP8_BLOCK + q * 32);
+                a[u][0] = ap[0];
+                a[u][1] = ap[1];
+                ea[u] = g.a_scales[(size_t)b * g.a_pitch + row];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            i32x8 fw, fa;
+            if constexpr (QUANT) {
+                unsigned top = 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if ((wave + u * WAVES) * FP8_BLOCK + q * 32 + j * 8 >= g.k) a[u][j] = u32x4{0u, 0u, 0u, 0u};   // zeros behind k
+                    top = max(top, bf16_amax(a[u][j]));
+                }
+                if (__builtin_amdgcn_ballot_w64(top >= BF16_INF) != 0) {   // of the finite ones
+                    top = 0;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) top = max(top, bf16_amax_finite(a[u][j]));
+                }
+                top = max(top, (unsigned)__shfl_xor((int)top, 16, 64));
+                top = max(top, (unsigned)__shfl_xor((int)top, 32, 64));
+                ea[u] = fp8_scale_byte(top);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const u32x2 c = fp8_codes_of(a[u][j], ea[u]);
+                    fa[2 * j] = (int)c.x;
+                    fa[2 * j + 1] = (int)c.y;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) fa[e] = (int)a[u][e / 4][e % 4];
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) fw[e] = (int)w[u][e / 4][e % 4];
+            if (u < mine) acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw, fa, acc, 0, 0, 0, ew[u], 0, ea[u]);
+        }
+    }
+    red[wave][lane] = acc;
+    __syncthreads();
+    // lane (i, q) of the result: row i, columns 4 q .. 4 q + 3; the waves in order
+    if (wave != 0 || i >= g.m) return;
+#pragma unroll
+    for (int v = 1; v < WAVES; ++v) acc += red[v][lane];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (n0 + 4 * q + e < g.n) g.out[(size_t)i * g.n + n0 + 4 * q + e] = f32_to_bf16(acc[e]);
+}
+
+template <int WAVES, int U, bool QUANT>
+__global__ __launch_bounds__(WAVES * 64) void fp8_rows_kernel(const RowsArgs g) {
+    __shared__ f32x4 red[WAVES][64];
+    rows_tile<WAVES, U, QUANT>(g, red);
+}
+
 // The slices' sums, in order, eight columns of the flattened result a thread.
 __global__ __launch_bounds__(256) void fp8_sum_kernel(const float* __restrict__ partial, int split, long count, bf16_t* __restrict__ out) {
     const long i = ((long)blockIdx.x * 256 + threadIdx.x) * 8;
@@ -382,9 +476,80 @@ int launch_tile(const Fp8Args& g, hipStream_t s) {
     return g.split > 1 ? launch<BM, BN, WM, WN, true, false>(g, s) : launch<BM, BN, WM, WN, false, false>(g, s);
 }
 
-struct TileDef { int bm, bn; };
-constexpr TileDef kTiles[] = {{64, 128}, {64, 256}, {128, 128}, {128, 256}, {192, 256}, {256, 128}, {256, 192}, {256, 256}};   // index = Fp8Plan::cfg
-constexpr int kNumTiles = sizeof(kTiles) / sizeof(kTiles[0]);
+template <bool QUANT>
+int launch_rows(const RowsArgs& g, hipStream_t s) {
+    const int blocks = g.columns / FP8_BLOCK;
+    const dim3 grid((g.n + 15) / 16);
+    // As few waves as hold all blocks at once; 16 columns, 1 row, us (waves, blocks a wave): 512 x 256 2.0 (4, 1), 2.4 (16, 1); 1000 x 1024
+    // 2.9 (8, 1), 3.3 (4, 2); 2048 x 2048 3.8 (16, 1), 4.9 (8, 4); 3584 x 3584 5.4 (16, 2), 5.6 (8, 4).
+    if (blocks <= 4) hipLaunchKernelGGL((fp8_rows_kernel<4, 1, QUANT>), grid, dim3(256), 0, s, g);
+    else if (blocks <= 8) hipLaunchKernelGGL((fp8_rows_kernel<8, 1, QUANT>), grid, dim3(512), 0, s, g);
+    else if (blocks <= 16) hipLaunchKernelGGL((fp8_rows_kernel<16, 1, QUANT>), grid, dim3(1024), 0, s, g);
+    else if (blocks <= 32) hipLaunchKernelGGL((fp8_rows_kernel<16, 2, QUANT>), grid, dim3(1024), 0, s, g);
+    else {
+        laps_set_error("gemm_fp8: %d blocks of k are too many for the kernel of few rows", blocks);
+        return LAPS_EINVAL;
+    }
+    LAPS_LAUNCH_CHECK();
+    return LAPS_OK;
+}
+
+// fill, slab: microseconds a workgroup takes besides its slabs, and for one; part: share of the slabs' time that goes away on an empty chip;
+// pair: time of two workgroups on a compute unit over that of two alone (0: one fits); live: share of the slabs' time that rows of
+// nothing spare.  Fitted, with the constants of laps_fp8_plan, to 6300 launches above 128 rows (15 weights from 512 x 12800 to 55296 x 5120, cold, at
+// 15 row counts to 4096, every tile and up to 20 slices): 9 % rms; the plans are 1.5 % behind the best one measured in the mean, 15 of
+// 223 products more than 10 % (573 x 7168 x 5120 41 us instead of 34).
+struct TileDef {
+    int bm, bn;
+    float fill, slab, part, pair, live;
+};
+constexpr TileDef kTiles[] = {
+    {64, 128, 2.00f, 0.395f, 0.18f, 0.86f, 0.01f},    // 0: 4 waves of 32 x 64
+    {64, 256, 1.95f, 0.633f, 0.12f, 1.00f, 0.00f},    // 1: of 64 x 64; up to 64 rows only
+    {128, 128, 2.57f, 0.486f, 0.20f, 1.00f, 0.00f},   // 2: of 64 x 64
+    {128, 256, 4.68f, 0.860f, 0.29f, 0.00f, 0.00f},   // 3: of 128 x 64
+    {192, 256, 6.56f, 1.026f, 0.21f, 0.00f, 0.07f},   // 4: of 96 x 128
+    {256, 128, 5.12f, 0.792f, 0.16f, 0.00f, 0.26f},   // 5: of 128 x 64
+    {256, 192, 6.77f, 1.027f, 0.16f, 0.00f, 0.20f},   // 6: of 64 x 192
+    {256, 256, 8.56f, 1.273f, 0.19f, 0.00f, 0.15f},   // 7: of 128 x 128
+    {16, 16, 0.f, 0.f, 0.f, 0.f, 0.f},                // 8: fp8_rows_kernel
+};
+constexpr int kNumTiles = sizeof(kTiles) / sizeof(kTiles[0]), kRowsCfg = 8;
+constexpr size_t kPartialCap = (size_t)256 << 20;   // bytes of an automatic split's sums
+
+long tiles_of(int cfg, int m, int n) { return ((long)m + kTiles[cfg].bm - 1) / kTiles[cfg].bm * (((long)n + kTiles[cfg].bn - 1) / kTiles[cfg].bn); }
+
+// Up to 128 rows: the weights' stream, and for narrow ones the latency of a few slabs.
+Fp8Plan few_rows_plan(int m, int n, int blocks) {
+    auto plan = [&](int cfg, long split) {
+        while (split > 1 && (size_t)split * m * n * sizeof(float) > kPartialCap) --split;
+        split = std::max(1L, split);
+        const int per = (int)((blocks + split - 1) / split);
+        return Fp8Plan{cfg, (blocks + per - 1) / per, per};
+    };
+    // Up to 16 rows of weights that fit the chip in one go: one launch without sums (1 row of codes, us, with / without this kernel: 3584 x 3584
+    // 5.4 / 7.1, 2048 x 2048 3.8 / 6.0, 512 x 256 2.0 / 3.1, 8192 x 2048 6.1 / 7.4, 16384 x 512 3.8 / 4.3; beyond the line 4608 x 3584 8.0 / 7.5,
+    // 5120 x 5120 12.7 / 8.8, 37888 x 3584 30 / 27).
+    const long narrow = (n + 15L) / 16;
+    if (m <= 16 && blocks <= 32 && narrow * blocks <= 8192 && (blocks <= 16 || narrow <= 256)) return {kRowsCfg, 1, blocks};
+    const long tiles = (n + 127L) / 128, wide = (n + 255L) / 256;
+    // A unit takes in A beside the weights, so the widest tile that still gives every unit one; where columns are few, K slices, of 5
+    // slabs at least, which cost a launch and their sums (3 us) and pay from 20 slabs on (64 rows, us: 5120 x 5120 in 1 / 3 / 5 slices 22 / 15.4 /
+    // 13.7, 3584 x 18944 in 4 / 9 25.3 / 20.2, 9000 x 2048 in 1 / 3 10.5 / 11.9).
+    if (m <= 64) {
+        if (tiles <= 256) return plan(0, blocks >= 20 ? std::min(256 / tiles, blocks / 5L) : 1);
+        return plan(wide <= 256 ? 1 : 0, 1);
+    }
+    // 65 to 128 rows on half the chip's units at most: two tiles of 64 rows in slices of 9 slabs at least, while a slice is short enough that
+    // reading the weights twice does not show (128 rows: 5120 x 5120 13.9 on 64 rows in 3 slices, 16.8 on 128 in 6; 3584 x 18944 25.8 and 26.6;
+    // 5120 x 27648 48.9 in 3 and 40.0 in 6).
+    if (2 * tiles <= 256) {
+        const long split = blocks >= 20 ? std::max(1L, std::min(256 / (2 * tiles), blocks / 9L)) : 1;
+        if (blocks <= 48 * split) return plan(0, split);
+    }
+    if (tiles <= 256) return plan(2, blocks >= 20 ? std::min(256 / tiles, blocks / 9L) : 1);
+    return plan(wide <= 256 ? 3 : 2, 1);
+}
 
 }  // namespace
 
@@ -395,11 +560,36 @@ void laps_fp8_tile_dims(int cfg, int* bm, int* bn) {
 
 Fp8Plan laps_fp8_plan(int m, int n, int k) {
     const int blocks = k / FP8_BLOCK;
-    const int cfg = m <= 64 ? 0 : m <= 128 ? 2 : 7;
-    const long tiles = ((m + (long)kTiles[cfg].bm - 1) / kTiles[cfg].bm) * ((n + (long)kTiles[cfg].bn - 1) / kTiles[cfg].bn);
-    long split = std::max(1L, std::min(256 / tiles, (long)blocks / 4));
-    const int per = (int)((blocks + split - 1) / split);
-    return {cfg, (blocks + per - 1) / per, per};
+    if (m <= 128) return few_rows_plan(m, n, blocks);
+    // Above 128 rows: workgroups on the busiest unit times what one takes, not less than the weights take from HBM; a split adds a launch and
+    // its sums written and read back.
+    auto moved = [](double b) { return std::min(b, 64e6) / 6.66e6 + std::max(0.0, b - 64e6) / 10.9e6; };
+    const double mn = (double)m * n;
+    double best = 1e30;
+    Fp8Plan pick = {7, 1, blocks};
+    for (int cfg = 0; cfg < kRowsCfg; ++cfg) {
+        if (cfg == 1) continue;
+        const TileDef& t = kTiles[cfg];
+        const long tiles = tiles_of(cfg, m, n), rows = ((long)m + t.bm - 1) / t.bm;
+        const double slab = t.slab * (1 - t.live * (1 - (double)m / ((double)rows * t.bm)));
+        for (int s = 1; s <= 20 && s <= std::max(1, blocks / 2); ++s) {
+            const int per = (blocks + s - 1) / s;
+            if ((blocks + per - 1) / per != s) continue;
+            if (s > 1 && (tiles * s > 512 || 4.0 * s * mn > (double)kPartialCap)) break;
+            const long wgs = tiles * s, deep = (wgs + 255) / 256;
+            const double all = per * slab, last = (wgs - (deep - 1) * 256) / 256.0;
+            double us;
+            if (t.pair > 0) us = deep / 2 * (t.fill + 2 * t.pair * all) + deep % 2 * (t.fill + all * (1 - t.part * (1 - std::min(1.0, wgs / 256.0))));
+            else us = (deep - 1) * (t.fill + all) + t.fill + all * (1 - t.part * (1 - last));
+            us = 1.6 + std::max(us, 3.4 + (double)n * k / 3.8e6);
+            if (s > 1) us += 3.2 + moved(8.0 * s * mn + 2.0 * mn);
+            if (us < best) {
+                best = us;
+                pick = {cfg, s, per};
+            }
+        }
+    }
+    return pick;
 }
 
 int laps_launch_gemm_fp8(const Fp8Plan& p, const unsigned char* a, const unsigned char* a_scales, const unsigned char* w,
@@ -410,6 +600,7 @@ int laps_launch_gemm_fp8(const Fp8Plan& p, const unsigned char* a, const unsigne
         laps_set_error("gemm_fp8: no tile %d", p.cfg);
         return LAPS_EINVAL;
     }
+    if (p.cfg == kRowsCfg) return launch_rows<false>({a, a_scales, nullptr, w, w_scales, out, m, n, k, k, (int)fp8_pitch(m), (int)fp8_pitch(n)}, s);
     const Fp8Args g = {a, a_scales, w, w_scales, (int)fp8_pitch(m), (int)fp8_pitch(n), m, n, k, p.split, p.per, (m + bm - 1) / bm, (n + bn - 1) / bn,
                        out, partial};
     int rc = LAPS_EINVAL;
@@ -430,4 +621,14 @@ int laps_launch_gemm_fp8(const Fp8Plan& p, const unsigned char* a, const unsigne
         LAPS_LAUNCH_CHECK();
     }
     return LAPS_OK;
+}
+
+// Quantised on the way, where that beats a launch of its own: up to 8 rows, or a block a wave (3584 x 3584 at 1 / 4 / 16 rows 6.5 / 7.0 / 10.1 us, in
+// two launches 8.6 / 8.6 / 9.6; 2048 x 2048 at 16 5.8 and 7.4).
+bool laps_fp8_takes_bf16_rows(const Fp8Plan& p, const bf16_t* x, int m, int k) {
+    return p.cfg == kRowsCfg && (m <= 8 || p.per <= 16) && k % 8 == 0 && (reinterpret_cast<uintptr_t>(x) & 15) == 0;
+}
+
+int laps_launch_linear_fp8_rows(const bf16_t* x, const unsigned char* w, const unsigned char* w_scales, bf16_t* out, int m, int n, int k, hipStream_t s) {
+    return launch_rows<true>({nullptr, nullptr, x, w, w_scales, out, m, n, k, (int)fp8_columns(k), (int)fp8_pitch(m), (int)fp8_pitch(n)}, s);
 }

@@ -1,5 +1,6 @@
 """8-bit matrices on the GPU: quantised and read back bit for bit, products exactly where float32 sums are exact and within their roundings
 elsewhere, and a run of projections, cache and attention as a server would call them."""
+import ctypes as C
 import math
 
 import numpy as np
@@ -99,6 +100,12 @@ def exact(a, w):
     return O.value(*a) @ O.value(*w).T
 
 
+def plan(m, n, k):
+    out = (C.c_int32 * 5)()
+    assert api.lib().laps_gemm_fp8_plan_info(m, n, k, out) == 0
+    return out[0], out[1], out[2] > 1
+
+
 SHAPES = [(1, 1, 1), (1, 16, 128), (2, 3, 130), (17, 33, 129), (64, 64, 256), (65, 127, 640), (128, 128, 128), (129, 130, 384), (1, 512, 2048), (5, 1000, 1920),
           (96, 2560, 1152), (200, 320, 5120), (257, 511, 512), (300, 1031, 896), (16, 4608, 3584), (1, 3584, 18944), (3, 40, 12800), (700, 640, 1280),
           (1000, 2048, 256), (2300, 300, 384), (40, 9001, 256), (513, 2816, 640), (320, 4864, 128), (1500, 1800, 128)]
@@ -113,6 +120,34 @@ def test_products_of_whole_numbers_are_exact(ctx, m, n, k):
     got = product(ctx, a, w, out[:m * n].view(m, n))
     want = torch.from_numpy(exact(a, w)).to(torch.float32).to(torch.bfloat16)
     assert torch.equal(got.cpu(), want) and (out[m * n:] == 5).all()
+
+
+# Every tile, with and without K slices, on sizes that its edges cut.
+TILES = [(64, 33000, 130, (64, 256, False)), (645, 2965, 306, (128, 128, False)), (773, 129, 12004, (128, 128, True)), (100, 33000, 200, (128, 256, False)),
+         (1243, 3203, 1073, (128, 256, False)), (270, 3773, 13898, (128, 256, True)), (2291, 3616, 303, (192, 256, False)), (264, 5377, 12486, (192, 256, True)),
+         (552, 7277, 1222, (256, 128, False)), (131, 5691, 10588, (256, 128, True)), (1750, 6635, 487, (256, 192, False)), (2206, 541, 18307, (256, 192, True)),
+         (1559, 7785, 538, (256, 256, False)), (454, 8225, 8008, (256, 256, True)), (17, 102, 2455, (64, 128, True)), (16, 16384, 512, (16, 16, False)),
+         (9, 520, 512, (16, 16, False)), (3, 3584, 3300, (16, 16, False)), (16, 2100, 2048, (16, 16, False)), (16, 300, 1000, (16, 16, False))]
+
+
+@pytest.mark.parametrize("m,n,k,tile", TILES)
+def test_products_on_every_tile_are_exact(ctx, m, n, k, tile):
+    """As above, in 64 bits on the GPU."""
+    assert plan(m, n, k) == tile
+    g = torch.Generator(device="cuda").manual_seed(m + n)
+
+    def matrix(rows, small):
+        x = torch.zeros((rows, -(-k // 128) * 128), device="cuda")
+        x[:, :k] = torch.randint(-3, 4, (rows, k), device="cuda", generator=g).float()
+        scales = torch.randint(127, 128 + small, (x.shape[1] // 128, -(-rows // 16) * 16), dtype=torch.uint8, device="cuda", generator=g)
+        value = x.double().unflatten(1, (-1, 128)) * torch.exp2(scales.T[:rows].double() - 127)[..., None]
+        return x.to(torch.float8_e4m3fn).view(torch.uint8), scales, value.flatten(1)
+
+    (a, a_scales, va), (w, w_scales, vw) = matrix(m, 3), matrix(n, 2)
+    out = torch.full((m * n + 16,), 5.0, dtype=torch.bfloat16, device="cuda")
+    ctx.laps_gemm_fp8(a, a_scales, w, w_scales, out=out[:m * n].view(m, n))
+    want = (va @ vw.T.contiguous()).float().to(torch.bfloat16)
+    assert torch.equal(out[:m * n].view(m, n), want) and (out[m * n:] == 5).all()
 
 
 def test_every_k_counts_once_under_its_own_scale(ctx):
@@ -174,7 +209,8 @@ def test_scales_at_their_ends(ctx, e):
     assert (got == (math.inf if total > 2.0 ** 128 else total if total > 2.0 ** -126 else 0.0)).all()
 
 
-@pytest.mark.parametrize("m,n,k", [(1, 3584, 3584), (1, 7, 100), (37, 640, 1000), (130, 200, 5120), (600, 300, 72), (2, 9000, 130)])
+@pytest.mark.parametrize("m,n,k", [(1, 3584, 3584), (1, 7, 100), (37, 640, 1000), (130, 200, 5120), (600, 300, 72), (2, 9000, 130), (8, 2000, 4096), (8, 333, 3000),
+                                   (9, 2000, 4096), (16, 500, 2048), (16, 77, 1016), (5, 300, 1012), (3, 640, 40), (16, 4000, 512), (1, 8000, 136)])
 def test_linear_is_quantise_then_multiply(ctx, m, n, k):
     g = np.random.default_rng(k)
     x = torch.from_numpy(g.standard_normal((m, k)).astype(np.float32)).to(torch.bfloat16).cuda()
@@ -183,6 +219,27 @@ def test_linear_is_quantise_then_multiply(ctx, m, n, k):
     assert torch.equal(ctx.laps_linear_fp8(x, *w), want)
     padded = torch.nn.functional.pad(x, (0, w[0].shape[1] - k))
     assert torch.equal(ctx.laps_linear_fp8(padded, *w), want)
+
+
+@pytest.mark.parametrize("m,n,k", [(3, 200, 1032), (4, 64, 4096), (40, 64, 512)])
+def test_linear_of_values_that_are_not_finite(ctx, m, n, k):
+    """Quantised in one launch with the product or in one of its own: the scale is that of a block's finite values."""
+    g = np.random.default_rng(m)
+    x = bits_of(g, (m, k)) if k == 512 else torch.from_numpy(g.standard_normal((m, k)).astype(np.float32)).to(torch.bfloat16)
+    x[1, 130], x[m - 1, k - 1] = math.inf, math.nan
+    w = ctx.laps_fp8_quant(torch.from_numpy(g.standard_normal((n, k)).astype(np.float32)).to(torch.bfloat16).cuda())
+    got, want = ctx.laps_linear_fp8(x.cuda(), *w), ctx.laps_gemm_fp8(*ctx.laps_fp8_quant(x.cuda()), *w)
+    assert torch.isnan(got[1]).all() and torch.isnan(got[m - 1]).all() and torch.equal(got.view(torch.int16)[~torch.isnan(got)], want.view(torch.int16)[~torch.isnan(got)])
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+
+
+def test_linear_of_rows_off_their_bounds(ctx):
+    """Rows two bytes off 16-byte bounds take the launch that reads them one by one."""
+    g = torch.Generator(device="cuda").manual_seed(8)
+    flat = torch.empty(3 * 1024 + 1, dtype=torch.bfloat16, device="cuda").normal_(0, 1, generator=g)
+    w = ctx.laps_fp8_quant(torch.empty((500, 1024), dtype=torch.bfloat16, device="cuda").normal_(0, 1, generator=g))
+    x = flat[1:].view(3, 1024)
+    assert torch.equal(ctx.laps_linear_fp8(x, *w), ctx.laps_linear_fp8(x.clone(), *w))
 
 
 def test_results_repeat_on_any_stream(ctx):
