@@ -70,12 +70,18 @@ struct Piece<HD, true> {
 };
 
 // NR: blocks of 16 rows that share what is read and unpacked.
+// Waves a SIMD: as many as registers allow.  4 bits hold 3 (NR 1) and 2; 8 bits have twice the pieces of a step in registers.  With one
+// block they go two steps ahead at 2 waves rather than one step ahead at 3: 32B, 64 tokens over 4096 keys each 167 -> 145 us,
+// over 512 to 8191 130 -> 114 (the loads alone, without the work on them, take 92 of the first).  With two blocks 2 waves spill 25
+// registers inside the loop, and 1 wave is faster: 32B, 16 sequences of 4 / 16 tokens over 2048 keys 29.8 / 47.9 -> 21.3 / 44.1 us
+// (two steps ahead 22.0 / 46.2).
 template <int HD, int NR, bool KV8>
-__global__ __launch_bounds__(WAVES * 64, NR == 1 ? 3 : 2) void attn_rows_kernel(
+__global__ __launch_bounds__(WAVES * 64, (KV8 ? 3 : 4) - NR) void attn_rows_kernel(
     const bf16_t* __restrict__ q, bf16_t* __restrict__ out, const byte_t* __restrict__ k_pool, const byte_t* __restrict__ v_pool,
     const int* __restrict__ cu, const int* __restrict__ seq_len, const int* __restrict__ prefix_len,
     const int* __restrict__ page_table, int max_pages, int n_seq, int n_tokens, int n_q, int n_kv, int n_pool_pages, int row_blocks, int parts,
     int min_parts, float scale_log2e, float* __restrict__ part_o, float* __restrict__ part_ml) {
+    constexpr int AHEAD = KV8 && NR == 1 ? 2 : 1;   // steps whose loads are on their way behind the one that is worked on
     constexpr int KS = HD / 32;        // matrix instructions of a page's scores
     constexpr int DL = HD / 16;        // head_dim indices of a lane of V, and of the result's 16 rows each
     constexpr int BLOCK = kv4_block(HD), CODES = kv4_codes(HD), ROWS = 16 * NR;
@@ -97,7 +103,13 @@ __global__ __launch_bounds__(WAVES * 64, NR == 1 ? 3 : 2) void attn_rows_kernel(
     const int need = (kv_len + LAPS_PAGE - 1) / LAPS_PAGE, n_pages = need < max_pages ? need : max_pages;
     const int* pt = page_table + (size_t)seq * max_pages;
     const unsigned k_turn = (8 * (HD == 128 ? g : 2 * (i & 1) + (g >> 1)) + 9) & 31;   // right rotation that brings the lane's scale byte up
+    // 8-bit pools: a lane's places in a block, and that of the scales' dword from there (in a vector register: scalar loads return in any
+    // order, so that each wait for one is for those of the next step too)
+    [[maybe_unused]] const unsigned kv8_lane_k = i * HD + g * 16, kv8_lane_v = i * 64 + g * 16;
     [[maybe_unused]] const int kv8_turn = 8 * (kvh & 3);
+    [[maybe_unused]] unsigned kv8_lane_s = (n_kv - kvh) * kv8_codes(HD) + (kvh & ~3);
+    [[maybe_unused]] const int kv8_bytes = kv8_lane_s + 4;   // from the block to the end of that dword
+    asm volatile("" : "+v"(kv8_lane_s));
     const int v_chunk = HD == 128 ? i : i >> 1, v_group = i / (KV4_GROUP / DL), o_group = g * 4 * DL / KV4_GROUP;
 
     for (int rb = rb0; rb * ROWS < n_rows; rb += row_blocks) {
@@ -140,22 +152,25 @@ __global__ __launch_bounds__(WAVES * 64, NR == 1 ? 3 : 2) void attn_rows_kernel(
         // Up to 16 rows a sequence: keys are read once and past the caches, 2.3 GB 418 -> 378 us (6.0 TB/s; 280 MB that the memory-side cache
         // held from the call before 52 -> 58).  More rows: other blocks of theirs read the same keys.
         auto codes = [](const auto* from) { return NR == 1 ? __builtin_nontemporal_load(from) : *from; };
+        // 8-bit pools: steps past the last one go through descriptors of no bytes, which takes no request.
         auto load = [&](int n, Piece<HD, KV8>& x) {
+            [[maybe_unused]] const int bytes = n < n_steps ? kv8_bytes : 0;
             if ((n & 31) == 0) fetch_ids(n);
 #pragma unroll
             for (int p = 0; p < 2; ++p) {
                 const int page = __builtin_amdgcn_readlane(ids, 2 * (n & 31) + p);
-                if constexpr (KV8) {
-                    const size_t at = (size_t)page * kv8_page(n_kv, HD);
-                    const byte_t *kb = k_pool + at, *vb = v_pool + at;
-                    const int own = kvh * (kv8_codes(HD) / 16), scales = n_kv * (kv8_codes(HD) / 4) + kvh / 4;
+                if constexpr (KV8) {   // through descriptors of the block: its base in scalar registers, a lane's place in one vector register
+                    const size_t at = (size_t)page * kv8_page(n_kv, HD) + (size_t)kvh * kv8_codes(HD);
+                    auto block = [&](const byte_t* pool) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<byte_t*>(pool + at), 0, bytes, 0x00020000); };
+                    const __amdgpu_buffer_rsrc_t kb = block(k_pool), vb = block(v_pool);
+                    constexpr int PAST = NR == 1 ? 2 : 0;   // nt, as below
 #pragma unroll
                     for (int u = 0; u < HD / 64; ++u) {
-                        x.k[p][u] = codes(reinterpret_cast<const u32x4*>(kb) + own + i * (HD / 16) + u * 4 + g);
-                        x.v[p][u] = codes(reinterpret_cast<const u32x4*>(vb) + own + (16 * u + i) * 4 + g);
+                        x.k[p][u] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kb, kv8_lane_k + u * 64, 0, 0));
+                        x.v[p][u] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vb, kv8_lane_v + u * 1024, 0, PAST));
                     }
-                    x.ks[p] = reinterpret_cast<const unsigned*>(kb)[scales];
-                    x.vs[p] = reinterpret_cast<const unsigned*>(vb)[scales];
+                    x.ks[p] = __builtin_amdgcn_raw_buffer_load_b32(kb, kv8_lane_s, 0, 0);
+                    x.vs[p] = __builtin_amdgcn_raw_buffer_load_b32(vb, kv8_lane_s, 0, 0);
                 } else {
                     const size_t at = ((size_t)page * n_kv + kvh) * BLOCK;
                     const byte_t *kb = k_pool + at, *vb = v_pool + at;
@@ -311,13 +326,30 @@ __global__ __launch_bounds__(WAVES * 64, NR == 1 ? 3 : 2) void attn_rows_kernel(
         // with a branch round the loads every wait would be for all of them.
         if (n_steps > 0) {
             Piece<HD, KV8> x, y;
-            auto load_at = [&](int n, Piece<HD, KV8>& to) { load(n < n_steps ? n : n_steps - 1, to); };
+            [[maybe_unused]] Piece<HD, KV8> z;
+            auto load_at = [&](int n, Piece<HD, KV8>& to) { load(KV8 || n < n_steps ? n : n_steps - 1, to); };
             load_at(0, x);
 #pragma unroll
             for (int a = 0; a < NR; ++a)
 #pragma unroll
                 for (int kk = 0; kk < KS; ++kk) asm volatile("" : "+v"(qf[a][kk]));   // as ids: the loop must find Q arrived
-            for (int n = 0;;) {
+            if constexpr (AHEAD == 2) {
+                load_at(1, y);
+                for (int n = 0;;) {
+                    load_at(n + 2, z);
+                    __builtin_amdgcn_sched_barrier(0);
+                    compute(n, x);
+                    if (++n >= n_steps) break;
+                    load_at(n + 2, x);
+                    __builtin_amdgcn_sched_barrier(0);
+                    compute(n, y);
+                    if (++n >= n_steps) break;
+                    load_at(n + 2, y);
+                    __builtin_amdgcn_sched_barrier(0);
+                    compute(n, z);
+                    if (++n >= n_steps) break;
+                }
+            } else for (int n = 0;;) {
                 load_at(n + 1, y);
                 __builtin_amdgcn_sched_barrier(0);   // loads first: mixed with the work, their registers get copied behind waits
                 compute(n, x);
@@ -552,9 +584,12 @@ int launch_rows(const RowsAttn& a, const RowsPlan& p, float* part, hipStream_t s
 // split.  And rows count by their mean: a long turn among single tokens is walked block after block by the few workgroups of
 // a sequence (32B, 95 tokens over 512 to 8100 keys 98 us, a turn of 350 over 4000 65, both in one call 1620, in blocks 363; 7B,
 // 127 tokens 72, a turn of 900 100, both 3008, in blocks 334).
+// 8 bits: as many workgroups as there are rounds of one a unit decide, so that half of them are the limit (32B, 16 turns of 17 to 64
+// tokens over 512 to 4096 keys, 896 workgroups, 94 us here and 81 in blocks; 64 of 8 over 2000, 1024, 96 and 87), and all launches
+// of fewer than 256 blocks of 128 rows, for the reason above (7B, 20 of 8 to 40 tokens over 64 to 10000 keys 129 us).
 bool laps_attn_takes_rows(int bits, int n_seq, int n_tokens, int n_q, int n_kv) {
     const long rows = (long)n_tokens * (n_q / n_kv), blocks = (rows + 32L * n_seq - 1) / (32L * n_seq);
-    return rows <= 16L * n_seq || blocks * n_seq * n_kv <= 1024;
+    return rows <= 16L * n_seq || blocks * n_seq * n_kv <= (bits == 8 ? 512 : 1024) || (bits == 8 && (rows / 128 + n_seq) * n_kv < 256);
 }
 
 RowsPlan laps_attn_rows_plan(int bits, int n_seq, int n_tokens, int n_q, int n_kv, int max_pages) {
@@ -577,10 +612,14 @@ RowsPlan laps_attn_rows_plan(int bits, int n_seq, int n_tokens, int n_q, int n_k
     // the parts that the batch leaves it: 32B, 95 tokens over 100 to 2000 keys and one over 100000 274 in 2 parts, 114 in 16, with
     // which the same table without a long one takes 76 instead of 42.
     if (rounds <= 8) return {tiles, (int)blocks, 1, 1};
-    const long units = blocks * n_seq * n_kv, places = tiles == 1 ? 768 : 256;
+    const long units = blocks * n_seq * n_kv, places = tiles == 1 ? (bits == 8 ? 512 : 768) : 256;
     auto within = [](long n, long most) { return n < most ? (n > 1 ? n : 1) : most; };
     const long min_parts = within(within(places / units, rounds / 2), MAX_PARTS);
-    const long parts = within(within((tiles == 1 ? 1536 : 1024) / units, rounds / (tiles == 1 ? 16 : 10)), MAX_PARTS);
+    // 8 bits, one block of rows (two workgroups are resident a unit), at most 1 / 1024 / 1536 workgroups over all parts: 32B, 64 tokens over
+    // 4096 keys each 88 / 98 / 98 us, over 512 to 8191 117 / 128 / 114; 14B, 96 over 512 to 8191 164 / 164 / 180; 32B, 40 over 100 to 16000
+    // 163 / 127 / 141; two over 100000 in 51 by each.
+    const long more = tiles == 2 ? 1024 : bits == 4 ? 1536 : units < 512 ? 1024 : 1;
+    const long parts = within(within(more / units, rounds / (tiles == 1 ? 16 : 10)), MAX_PARTS);
     return {tiles, (int)blocks, (int)(parts > min_parts ? parts : min_parts), (int)min_parts};
 }
 
