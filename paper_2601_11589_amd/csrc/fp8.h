@@ -41,6 +41,17 @@ static __device__ __forceinline__ unsigned bf16_amax_finite(u32x4 x) {   // of t
     return top;
 }
 
+// The largest of the values that N (8 or 16) lanes side by side hold, in each of them: pairs, fours, then halves and rows mirrored.
+template <int N>
+static __device__ __forceinline__ unsigned fp8_lanes_max(unsigned x) {
+    auto most = [](unsigned a, unsigned b) { return a > b ? a : b; };
+    x = most(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x0b1, 15, 15, true));   // quad_perm 1 0 3 2
+    x = most(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x04e, 15, 15, true));   // quad_perm 2 3 0 1
+    x = most(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 15, 15, true));   // row_half_mirror
+    if (N == 16) x = most(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x140, 15, 15, true));   // row_mirror
+    return x;
+}
+
 // Codes of eight bf16 values under 2^(byte - 127): to nearest, ties to the even code, what is not finite to NaN.  The conversion makes
 // magnitudes of 464 and more NaN, which a scale below the highest never meets; under that one they are cut to 448 first.
 static __device__ __forceinline__ u32x2 fp8_codes_of(u32x4 x, int byte) {

@@ -16,23 +16,30 @@
 
 namespace {
 
+// Bytes of LDS for 64 of V's block: the threads of a token write, or read, a byte in each second of these, and with 64 they would meet in two
+// banks of the 64.
+constexpr int TURN = 72;
+
 template <int HD, bool SCATTER, bool STREAM>
 __global__ __launch_bounds__(2 * HD) void kv8_move_kernel(const int* __restrict__ cu, const int* __restrict__ start_pos,
                                                           const int* __restrict__ page_table, u32x4* __restrict__ k_tok,
                                                           u32x4* __restrict__ v_tok, unsigned char* __restrict__ k_pool,
                                                           unsigned char* __restrict__ v_pool, int n_seq, int n_tokens,
                                                           int max_pages, int n_kv, int n_pool_pages) {
-    constexpr int CPR = HD / 8, CODES = kv8_codes(HD), WAVES = 2 * HD / 64;
-    __shared__ __align__(16) unsigned char turn[CODES];
-    __shared__ unsigned red[2][WAVES];
+    constexpr int CPR = HD / 8, CODES = kv8_codes(HD);
+    __shared__ __align__(16) unsigned char turn[CODES / 64 * TURN];
+    __shared__ unsigned red[2][LAPS_PAGE];
     // Work items: the first item of sequence s is cu[s] / 16 + 2 s (a run of n tokens touches at most n / 16 + 2 pages), items that no
     // page needs return at once.
     const int item = blockIdx.x, head = blockIdx.y, tid = threadIdx.x;
     auto first_item = [&](int s) { return cu[s] / LAPS_PAGE + 2 * s; };
-    int lo = 0, hi = n_seq;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (first_item(mid) <= item) lo = mid; else hi = mid;
+    // A wave looks at 64 sequences at a time, one a lane.
+    int lo = 0;
+    for (int hi = n_seq; hi - lo > 1;) {
+        const int step = (hi - lo + 63) / 64, at = lo + (tid & 63) * step;
+        const int n = __popcll(__builtin_amdgcn_ballot_w64(at < hi && first_item(at < hi ? at : lo) <= item));
+        if (n > 1) lo += (n - 1) * step;
+        hi = lo + step < hi ? lo + step : hi;
     }
     // whatever the arrays hold: tokens stay in [0, n_tokens), pages in the table, page ids in the pool
     const int c0 = cu[lo], c1 = cu[lo + 1], t1 = c1 < n_tokens ? c1 : n_tokens;
@@ -55,8 +62,9 @@ __global__ __launch_bounds__(2 * HD) void kv8_move_kernel(const int* __restrict_
         if (STREAM) __builtin_nontemporal_store(x, to);
         else *to = x;
     };
-    // byte of (head_dim index 8 c + j, token t) in V's block
-    auto v_place = [&](int j) { return (2 * c + j / 4) * 64 + (t / 4) * 16 + (j % 4) * 4 + t % 4; };
+    // where V's block is turned over: byte of (head_dim index 8 c + j, token t), and this thread's eight bytes as they lie in the pool
+    auto v_place = [&](int j) { return (2 * c + j / 4) * TURN + (t / 4) * 16 + (j % 4) * 4 + t % 4; };
+    u32x2* turned = reinterpret_cast<u32x2*>(turn + tid / 8 * TURN + tid % 8 * 8);
     u32x2 *k8 = reinterpret_cast<u32x2*>(kb) + tid, *v8 = reinterpret_cast<u32x2*>(vb) + tid;   // this thread's eight bytes of each block
     if (SCATTER) {
         const bool keeps = off0 > 0;   // the page holds tokens that stay
@@ -75,31 +83,18 @@ __global__ __launch_bounds__(2 * HD) void kv8_move_kernel(const int* __restrict_
         }
         // largest magnitude of the token's head, and of the new tokens whose head is finite
         unsigned ka = bf16_amax(k), va = bf16_amax(v);
-#pragma unroll
-        for (int i = 1; i < CPR; i <<= 1) {
-            const unsigned ko = __shfl_xor(ka, i, 64), vo = __shfl_xor(va, i, 64);
-            ka = ko > ka ? ko : ka;
-            va = vo > va ? vo : va;
-        }
+        ka = fp8_lanes_max<CPR>(ka);
+        va = fp8_lanes_max<CPR>(va);
         const bool k_fine = ka < BF16_INF, v_fine = va < BF16_INF;
         ka = k_fine ? ka : 0u;
         va = v_fine ? va : 0u;
-#pragma unroll
-        for (int i = CPR; i < 64; i <<= 1) {
-            const unsigned ko = __shfl_xor(ka, i, 64), vo = __shfl_xor(va, i, 64);
-            ka = ko > ka ? ko : ka;
-            va = vo > va ? vo : va;
-        }
-        if ((tid & 63) == 0) {
-            red[0][tid >> 6] = ka;
-            red[1][tid >> 6] = va;
+        if (c == 0) {   // a word a token
+            red[0][t] = ka;
+            red[1][t] = va;
         }
         __syncthreads();
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            ka = red[0][w] > ka ? red[0][w] : ka;
-            va = red[1][w] > va ? red[1][w] : va;
-        }
+        ka = fp8_lanes_max<16>(red[0][tid & 15]);
+        va = fp8_lanes_max<16>(red[1][tid & 15]);
         int kn = fp8_scale_byte(ka), vn = fp8_scale_byte(va);
         if (keeps) {
             kn = ks_old > kn ? ks_old : kn;
@@ -119,7 +114,7 @@ __global__ __launch_bounds__(2 * HD) void kv8_move_kernel(const int* __restrict_
         unsigned fresh = 0;   // bytes of a dword that are new
 #pragma unroll
         for (int e = 0; e < 4; ++e) fresh |= 4 * g + e >= off0 && 4 * g + e < off1 ? 255u << (8 * e) : 0u;
-        u32x2 out = reinterpret_cast<const u32x2*>(turn)[tid];
+        u32x2 out = *turned;
         if (keeps && fresh != ~0u) {
             const u32x2 stay = again(v_old, vs_old, vn);
             out = u32x2{(out.x & fresh) | (stay.x & ~fresh), (out.y & fresh) | (stay.y & ~fresh)};
@@ -132,7 +127,7 @@ __global__ __launch_bounds__(2 * HD) void kv8_move_kernel(const int* __restrict_
     } else {
         const u32x2 kc = *k8, vc = *v8;
         const float kf = fp8_scale(*ks), vf = fp8_scale(*vs);
-        reinterpret_cast<u32x2*>(turn)[tid] = vc;
+        *turned = vc;
         __syncthreads();
         if (!mine) return;
         put(fp8_eight(kc.x, kc.y, kf), k_tok + at);
