@@ -21,7 +21,7 @@ struct RowsPlan {
     int min_parts;    // as many at least, where there are keys for them
 };
 // Which of the two kernels a launch shape takes: this one, or the blocks of 128 or 256 rows of the bf16 pools' attention.
-bool laps_attn_takes_rows(int bits, int n_seq, int n_tokens, int n_q, int n_kv);
+bool laps_attn_takes_rows(int n_seq, int n_tokens, int n_q, int n_kv);
 RowsPlan laps_attn_rows_plan(int bits, int n_seq, int n_tokens, int n_q, int n_kv, int max_pages);
 size_t laps_attn_rows_bytes(const RowsPlan& p, int n_tokens, int n_q, int hd);   // partial results of the parts
 int laps_launch_attn_rows(const RowsAttn& a, const RowsPlan& p, float* partial, hipStream_t s);

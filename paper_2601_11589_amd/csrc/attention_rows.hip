@@ -69,14 +69,46 @@ struct Piece<HD, true> {
     unsigned ks[2], vs[2];           // the page's scale bytes, each in a dword of four kv heads'
 };
 
+// O += V^T P^T.  8-bit pools: by hand, with one operand for what O was and what it is.  The builtin has two, and with twice the pieces of a
+// step in registers the allocator no longer gets by without moves and spills: two blocks of rows 25 spills at 2 waves a SIMD, now none.
+// The compiler does not know what such an instruction needs before and behind it: the two wait states behind vector instructions that
+// made its operands stand here, those before O is used otherwise are o_settle's.
+template <bool KV8>
+__device__ __forceinline__ void add_product(f32x4& o, bf16x8 v, bf16x8 p) {
+    if constexpr (KV8) asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(o) : "v"(v), "v"(p));
+    else o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p, o, 0, 0, 0);
+}
+template <bool KV8, int NR, int DL>
+__device__ __forceinline__ void o_settle(f32x4 (&o)[NR][DL]) {
+    if constexpr (KV8) {
+        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+#pragma unroll
+        for (int a = 0; a < NR; ++a)
+#pragma unroll
+            for (int j = 0; j < DL; ++j) asm volatile("" : "+v"(o[a][j]));
+    }
+}
+
+// 8-bit pools, several blocks of rows: those of a (sequence, part, kv head) read the same keys and go to one XCD one after the other, in n
+// groups where there are too few of these for the 8 XCDs to share evenly.  Against kv heads side by side, which 4-bit blocks want (they
+// share lines): 32B, 64 sequences of 16 tokens over 2000 keys 113 -> 94 us, 16 of 64 over 2048 88 -> 76, 7B, two of 17 over 60000 81 -> 64.
+struct RowsGroups {
+    int n, blocks;   // blocks of a group
+    __host__ __device__ RowsGroups(int units, int row_blocks) {
+        n = (64 + units - 1) / units;
+        n = n < row_blocks ? n : row_blocks;
+        blocks = (row_blocks + n - 1) / n;
+    }
+};
+
 // NR: blocks of 16 rows that share what is read and unpacked.
-// Waves a SIMD: as many as registers allow.  4 bits hold 3 (NR 1) and 2; 8 bits have twice the pieces of a step in registers.  With one
-// block they go two steps ahead at 2 waves rather than one step ahead at 3: 32B, 64 tokens over 4096 keys each 167 -> 145 us,
-// over 512 to 8191 130 -> 114 (the loads alone, without the work on them, take 92 of the first).  With two blocks 2 waves spill 25
-// registers inside the loop, and 1 wave is faster: 32B, 16 sequences of 4 / 16 tokens over 2048 keys 29.8 / 47.9 -> 21.3 / 44.1 us
-// (two steps ahead 22.0 / 46.2).
+// Waves a SIMD: as many as registers allow, 3 (4 bits, one block) or 2.  8 bits have twice the pieces of a step in registers; with one block
+// they go two steps ahead at 2 waves rather than one step ahead at 3: 32B, 64 tokens over 4096 keys each 112 -> 98 us, over 512 to
+// 8191 130 -> 114 (the loads alone, without the work on them, take 92 of the first).
+// Four blocks that share what is unpacked, at one wave a SIMD, are not kept: 32B, 16 sequences of 17 to 64 tokens over 512 to 4096 keys
+// 88 us and, with the next step's scores among this one's exponentials, 92; two blocks 78.
 template <int HD, int NR, bool KV8>
-__global__ __launch_bounds__(WAVES * 64, (KV8 ? 3 : 4) - NR) void attn_rows_kernel(
+__global__ __launch_bounds__(WAVES * 64, NR == 1 && !KV8 ? 3 : 2) void attn_rows_kernel(
     const bf16_t* __restrict__ q, bf16_t* __restrict__ out, const byte_t* __restrict__ k_pool, const byte_t* __restrict__ v_pool,
     const int* __restrict__ cu, const int* __restrict__ seq_len, const int* __restrict__ prefix_len,
     const int* __restrict__ page_table, int max_pages, int n_seq, int n_tokens, int n_q, int n_kv, int n_pool_pages, int row_blocks, int parts,
@@ -90,8 +122,18 @@ __global__ __launch_bounds__(WAVES * 64, (KV8 ? 3 : 4) - NR) void attn_rows_kern
 
     // Workgroup b runs on XCD b % 8.  The kv heads of a (sequence, part, row block) go to one XCD side by side: a page's heads are
     // neighbours in memory and a block is 8.5 (4.25) lines of 128 bytes, so that each fetches a line that the next one needs too.
-    const int G = n_q / n_kv, kvh = blockIdx.x / 8 % n_kv, rest = blockIdx.x / 8 / n_kv * 8 + blockIdx.x % 8;
-    const int rb0 = rest % row_blocks, part = rest / row_blocks % parts, seq = rest / row_blocks / parts;
+    const int G = n_q / n_kv;
+    int kvh = blockIdx.x / 8 % n_kv, rest = blockIdx.x / 8 / n_kv * 8 + blockIdx.x % 8, rb0 = rest % row_blocks;
+    rest /= row_blocks;
+    if constexpr (KV8 && NR > 1) {
+        const RowsGroups grp(n_seq * parts * n_kv, row_blocks);
+        const int at = blockIdx.x / 8, unit = at / grp.blocks * 8 + blockIdx.x % 8;
+        rb0 = unit % grp.n + at % grp.blocks * grp.n;
+        if (rb0 >= row_blocks) return;
+        kvh = unit / grp.n % n_kv;
+        rest = unit / grp.n / n_kv;
+    }
+    const int part = rest % parts, seq = rest / parts;
     if (seq >= n_seq) return;
     SeqRange r;
     if (!seq_range(seq, cu, seq_len, prefix_len, n_tokens, max_pages, &r)) return;
@@ -263,6 +305,7 @@ __global__ __launch_bounds__(WAVES * 64, (KV8 ? 3 : 4) - NR) void attn_rows_kern
                 move = move || sum[a] > MOST || m_run[a] == -INFINITY;
             }
             if (__builtin_amdgcn_ballot_w64(move) != 0) {
+                o_settle<KV8>(o);
 #pragma unroll
                 for (int a = 0; a < NR; ++a) {
                     float mx = fmaxf(fmaxf(fmaxf(s[a][0].x, s[a][0].y), fmaxf(s[a][0].z, s[a][0].w)),
@@ -287,7 +330,7 @@ __global__ __launch_bounds__(WAVES * 64, (KV8 ? 3 : 4) - NR) void attn_rows_kern
                     const u32x2 lo = fp8_four(x.v[0][j / 4][j % 4], vs0), hi = fp8_four(x.v[1][j / 4][j % 4], vs1);
                     const bf16x8 vf = __builtin_bit_cast(bf16x8, u32x4{lo.x, lo.y, hi.x, hi.y});
 #pragma unroll
-                    for (int a = 0; a < NR; ++a) o[a][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[a], o[a][j], 0, 0, 0);
+                    for (int a = 0; a < NR; ++a) add_product<KV8>(o[a][j], vf, pf[a]);
                 }
             } else {
                 // codes of one head_dim pair of the eight keys, then the keys side by side
@@ -361,6 +404,7 @@ __global__ __launch_bounds__(WAVES * 64, (KV8 ? 3 : 4) - NR) void attn_rows_kern
             }
         }
 
+        o_settle<KV8>(o);
         // ---- NaN groups of keys that not every row sees
         nan_key = min(nan_key, __shfl_xor(nan_key, 16, 64));
         nan_key = min(nan_key, __shfl_xor(nan_key, 32, 64));
@@ -554,7 +598,13 @@ int launch_rows(const RowsAttn& a, const RowsPlan& p, float* part, hipStream_t s
     const float scale_log2e = 1.4426950408889634f / sqrtf((float)HD);
     float* part_ml = part ? part + (size_t)a.n_tokens * a.n_q * p.parts * HD : nullptr;
     auto kern = p.row_tiles == 1 ? attn_rows_kernel<HD, 1, KV8> : attn_rows_kernel<HD, 2, KV8>;
-    hipLaunchKernelGGL(kern, dim3((a.n_seq * p.parts * p.row_blocks + 7) / 8 * 8 * a.n_kv), dim3(WAVES * 64), 0, s, a.q, a.out, a.k_pool,
+    int wgs = (a.n_seq * p.parts * p.row_blocks + 7) / 8 * 8 * a.n_kv;
+    if (KV8 && p.row_tiles > 1) {
+        const int units = a.n_seq * p.parts * a.n_kv;
+        const RowsGroups grp(units, p.row_blocks);
+        wgs = (units * grp.n + 7) / 8 * 8 * grp.blocks;
+    }
+    hipLaunchKernelGGL(kern, dim3(wgs), dim3(WAVES * 64), 0, s, a.q, a.out, a.k_pool,
                        a.v_pool, a.cu, a.seq_len, a.prefix_len, a.page_table, a.max_pages, a.n_seq, a.n_tokens, a.n_q, a.n_kv, a.n_pool_pages,
                        p.row_blocks, p.parts, p.min_parts, scale_log2e, part, part_ml);
     LAPS_LAUNCH_CHECK();
@@ -584,12 +634,11 @@ int launch_rows(const RowsAttn& a, const RowsPlan& p, float* part, hipStream_t s
 // split.  And rows count by their mean: a long turn among single tokens is walked block after block by the few workgroups of
 // a sequence (32B, 95 tokens over 512 to 8100 keys 98 us, a turn of 350 over 4000 65, both in one call 1620, in blocks 363; 7B,
 // 127 tokens 72, a turn of 900 100, both 3008, in blocks 334).
-// 8 bits: as many workgroups as there are rounds of one a unit decide, so that half of them are the limit (32B, 16 turns of 17 to 64
-// tokens over 512 to 4096 keys, 896 workgroups, 94 us here and 81 in blocks; 64 of 8 over 2000, 1024, 96 and 87), and all launches
-// of fewer than 256 blocks of 128 rows, for the reason above (7B, 20 of 8 to 40 tokens over 64 to 10000 keys 129 us).
-bool laps_attn_takes_rows(int bits, int n_seq, int n_tokens, int n_q, int n_kv) {
+// 8 bits, this kernel / blocks: 32B, 16 sequences of 17 to 64 tokens over 512 to 4096 keys 78 / 81 us, 16 of 64 over 2048 76 / 81, 64 of 8 / 16 /
+// 32 over 2000 71 / 94 / 144 and 87 / 95 / 152, 4 of 200 over 16000 359 / 294; 7B, 12 of 60 to 120 over 100 to 3000 75 / 72.
+bool laps_attn_takes_rows(int n_seq, int n_tokens, int n_q, int n_kv) {
     const long rows = (long)n_tokens * (n_q / n_kv), blocks = (rows + 32L * n_seq - 1) / (32L * n_seq);
-    return rows <= 16L * n_seq || blocks * n_seq * n_kv <= (bits == 8 ? 512 : 1024) || (bits == 8 && (rows / 128 + n_seq) * n_kv < 256);
+    return rows <= 16L * n_seq || blocks * n_seq * n_kv <= 1024;
 }
 
 RowsPlan laps_attn_rows_plan(int bits, int n_seq, int n_tokens, int n_q, int n_kv, int max_pages) {

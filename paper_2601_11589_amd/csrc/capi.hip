@@ -680,7 +680,7 @@ static WsLayout kvq_layout(int n_seq, int n_tokens, int n_q, int n_kv, int hd, i
 
 static size_t kvq_workspace_bytes(int bits, int n_seq, int n_tokens, int n_q, int n_kv, int hd, int max_pages) {
     if (n_seq < 1 || n_tokens < 1 || max_pages < 1 || max_pages > LAPS_KVQ_MAX_PAGES || (long)n_seq * n_q > LAPS_KVQ_MAX_SEQ_HEADS) return 0;
-    if (!laps_attn_takes_rows(bits, n_seq, n_tokens, n_q, n_kv)) return kvq_layout(n_seq, n_tokens, n_q, n_kv, hd, max_pages).total;
+    if (!laps_attn_takes_rows(n_seq, n_tokens, n_q, n_kv)) return kvq_layout(n_seq, n_tokens, n_q, n_kv, hd, max_pages).total;
     return align256(laps_attn_rows_bytes(laps_attn_rows_plan(bits, n_seq, n_tokens, n_q, n_kv, max_pages), n_tokens, n_q, hd) + 1);
 }
 
@@ -694,7 +694,7 @@ static int kvq_plan_info(const char* who, int bits, int n_seq, int n_tokens, int
         return LAPS_EINVAL;
     }
     out[5] = (int64_t)bytes;
-    if (laps_attn_takes_rows(bits, n_seq, n_tokens, n_q_heads, n_kv_heads)) {
+    if (laps_attn_takes_rows(n_seq, n_tokens, n_q_heads, n_kv_heads)) {
         const RowsPlan p = laps_attn_rows_plan(bits, n_seq, n_tokens, n_q_heads, n_kv_heads, max_pages);
         out[0] = 16 * p.row_tiles;
         out[1] = p.row_blocks;
@@ -737,7 +737,7 @@ static int attention_kvq(const char* who, int bits, laps_ctx* c, int n_seq, int 
         return LAPS_ENOMEM;
     }
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (laps_attn_takes_rows(bits, n_seq, n_tokens, cf.n_q_heads, cf.n_kv_heads)) {
+    if (laps_attn_takes_rows(n_seq, n_tokens, cf.n_q_heads, cf.n_kv_heads)) {
         const RowsAttn a = {static_cast<const bf16_t*>(q), static_cast<bf16_t*>(out), static_cast<const unsigned char*>(k_pool),
                             static_cast<const unsigned char*>(v_pool), cu, seq_len, prefix_len, pt, n_seq, n_tokens, max_pages,
                             n_pages, cf.n_q_heads, cf.n_kv_heads, cf.head_dim, bits};
