@@ -620,6 +620,13 @@ class LapsCtx:
         return y
 
     # ---- 8-bit matrices
+    def _fp8_pitch(self, what, rows):
+        """Bytes of a block's scales; refuses counts that the library's 32 bits would cut."""
+        pitch = lib().laps_fp8_scale_pitch(rows)
+        if pitch == 0:
+            raise LapsError(f"{what}: {rows} rows")
+        return pitch
+
     def _fp8_matrix(self, what, codes, scales, k, device):
         """Checks codes [rows, k rounded up to 128] and their scales: returns rows and addresses."""
         rows, columns = codes.shape[0], lib().laps_fp8_columns(k)
@@ -630,10 +637,10 @@ class LapsCtx:
         """bf16 [rows, k] -> 8-bit floats (uint8 [rows, k rounded up to 128], zeros behind k; views as torch.float8_e4m3fn) and their scale
         bytes (uint8 [blocks of 128, rows rounded up to 16])."""
         (rows, k), device = x.shape, x.get_device()
-        columns = lib().laps_fp8_columns(k)
+        columns, pitch = lib().laps_fp8_columns(k), self._fp8_pitch("x", rows)
         x_p = _expect("x", x, torch.bfloat16, (rows, k), device)
         codes = torch.empty((rows, columns), dtype=torch.uint8, device=x.device) if codes is None else codes
-        scales = torch.empty((columns // 128, lib().laps_fp8_scale_pitch(rows)), dtype=torch.uint8, device=x.device) if scales is None else scales
+        scales = torch.empty((columns // 128, pitch), dtype=torch.uint8, device=x.device) if scales is None else scales
         _, codes_p, scales_p = self._fp8_matrix("codes", codes, scales, k, device)
         if codes.shape[0] != rows:
             raise LapsError(f"codes: need {rows} rows, got {codes.shape[0]}")
@@ -670,6 +677,7 @@ class LapsCtx:
     def laps_linear_fp8(self, x, w, w_scales, out=None, stream=None):
         """bf16 [m, n] = x w^T: laps_fp8_quant of the bf16 rows x [m, k], then laps_gemm_fp8."""
         (m, k), device = x.shape, w.get_device()
+        self._fp8_pitch("x", m)
         x_p = _expect("x", x, torch.bfloat16, (m, k), device)
         n, w_p, ws_p = self._fp8_matrix("w", w, w_scales, k, device)
         y = torch.empty((m, n), dtype=torch.bfloat16, device=w.device) if out is None else out

@@ -242,6 +242,46 @@ def test_linear_of_rows_off_their_bounds(ctx):
     assert torch.equal(ctx.laps_linear_fp8(x, *w), ctx.laps_linear_fp8(x.clone(), *w))
 
 
+@pytest.mark.parametrize("m", [2, 40, 200])
+def test_long_offsets(ctx, m):
+    """Weights and rows behind 4 GiB: their last columns and rows against the same ones in matrices of their own."""
+    n, k = (1 << 20) + 77, 4224
+    g = torch.Generator(device="cuda").manual_seed(m)
+    tail = torch.empty((77, k), dtype=torch.bfloat16, device="cuda").normal_(0, 1, generator=g)
+    x = torch.empty((m, k), dtype=torch.bfloat16, device="cuda").normal_(0, 1, generator=g)
+    few = ctx.laps_fp8_quant(tail)
+    if m == 2:   # rows behind 4 GiB: of 8-bit codes and, twice as far, of bf16
+        wide_w = torch.zeros((n, k), dtype=torch.bfloat16, device="cuda")
+        wide_w[-77:] = tail
+        codes, scales = ctx.laps_fp8_quant(wide_w)
+        assert torch.equal(codes[-77:], few[0]) and torch.equal(scales[:, n - 77:n], few[1][:, :77]) and not codes[:-77].any()
+        wide_w.fill_(3)
+        ctx.laps_fp8_dequant(codes, scales, k, wide_w)
+        assert torch.equal(wide_w[-77:], ctx.laps_fp8_dequant(*few, k)) and not wide_w[:-77].any()
+        del wide_w
+    else:
+        codes = torch.zeros((n, k), dtype=torch.uint8, device="cuda")
+        scales = torch.full((k // 128, (n + 15) // 16 * 16), 127, dtype=torch.uint8, device="cuda")
+        codes[-77:], scales[:, n - 77:n] = few[0], few[1][:, :77]
+    got = ctx.laps_linear_fp8(x, codes, scales)
+    vx, vw = (ctx.laps_fp8_dequant(*q, k).double() for q in (ctx.laps_fp8_quant(x), few))
+    want, size = vx @ vw.T, vx.abs() @ vw.abs().T
+    groups = vx.abs().unflatten(1, (-1, 8)).amax(2) @ vw.abs().unflatten(1, (-1, 8)).amax(2).T
+    assert not got[:, :-77].any()
+    slack = ULP * want.abs() + (1 + ULP) * (8 * 2.0 ** -13 * groups + (k / 8 + 64) * 2.0 ** -23 * size)   # as above
+    assert ((got[:, -77:].double() - want).abs() <= slack).all()
+
+
+def test_more_rows_than_the_library_counts(ctx):
+    """2^32 + 5 rows are not 5."""
+    x = torch.empty(((1 << 32) + 5, 1), dtype=torch.bfloat16, device="cuda")
+    w = ctx.laps_fp8_quant(torch.ones((1, 1), dtype=torch.bfloat16, device="cuda"))
+    with pytest.raises(api.LapsError, match="rows"):
+        ctx.laps_linear_fp8(x, *w)
+    with pytest.raises(api.LapsError, match="codes|rows"):
+        ctx.laps_fp8_quant(x)
+
+
 def test_results_repeat_on_any_stream(ctx):
     g = np.random.default_rng(3)
     a, w = O.quantise(g.standard_normal((48, 5120))), O.quantise(g.standard_normal((512, 5120)))

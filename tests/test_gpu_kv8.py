@@ -235,6 +235,20 @@ def test_head_layouts(heads):
     b.ctx.close()
 
 
+# Blocks of 32 rows that share keys, dealt to the XCDs in groups where (sequence, part, kv head) are few: 1 unit, 2, 3, 8 and many, blocks that
+# fill their groups and that do not
+@pytest.mark.parametrize("heads,new,pre", [((16, 1, 128), [100], [300]), ((16, 1, 128), [33, 70, 2], [5, 900, 64]), ((4, 2, 64), [200], [100]),
+                                           ((40, 8, 128), [90], [2500]), ((28, 4, 128), [5] * 9, [100, 0, 700, 64, 65, 31, 32, 33, 1]),
+                                           ((40, 8, 128), [13, 1, 40, 0, 7, 22, 9], [70, 300, 0, 5, 1900, 16, 15])])
+def test_row_blocks_of_the_same_keys(heads, new, pre):
+    n_q, n_kv, hd = heads
+    b = Batch(inputs.ModelCfg(256, n_q, n_kv, hd, 512, 1), new, pre, spare=3, seed=n_q + len(new)).write()
+    p = plan(b)
+    assert p[0] == 32 and p[1] > 1, p
+    b.check(b.attend())
+    b.ctx.close()
+
+
 # Batches large enough for the kernels of 128 and 256 rows, 64 query heads over 8: (new, prefix, spare pages, rows a workgroup, shares)
 BLOCKS = {
     "shares": ([300, 40, 260], [1500, 200, 0], 2, 256, True),
