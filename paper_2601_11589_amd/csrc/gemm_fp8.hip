@@ -11,6 +11,9 @@
 // of a half slab are in registers before its products begin, so a place is free again half a slab after it was waited for; one
 // barrier per half slab waits for the one that is needed next, never for all loads in flight.  Scale bytes lie [block][row], so those of
 // a tile are a few hundred bytes side by side for each slab; each wave fetches one slab's of the next four.
+//
+// Measured, us: 2048 x 55296 x 5120 443 to 463 (2.5 to 2.6 PFLOP/s: the matrix pipe is busy 68 % of the time at 1.6 GHz, the clock under these
+// operands), 96 x 55296 x 5120 53 (5.3 TB/s), 573 x 3584 x 18944 in six slices 43 and 8 for their sums.
 #include <algorithm>
 #include <type_traits>
 
