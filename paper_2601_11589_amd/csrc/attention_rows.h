@@ -17,6 +17,7 @@ struct RowsAttn {
 struct RowsPlan {
     int row_tiles;    // 16-row tiles of a block
     int row_blocks;   // blocks of rows that workgroups of their own walk, a sequence and kv head
+    int more_rows;    // as many times that, the last ones first in the launch
     int parts;        // most parts of a sequence's keys
     int min_parts;    // as many at least, where there are keys for them
 };

@@ -116,8 +116,8 @@ template <int HD, int NR, bool KV8>
 __global__ __launch_bounds__(WAVES * 64, NR == 1 && !KV8 ? 3 : 2) void attn_rows_kernel(
     const bf16_t* __restrict__ q, bf16_t* __restrict__ out, const byte_t* __restrict__ k_pool, const byte_t* __restrict__ v_pool,
     const int* __restrict__ cu, const int* __restrict__ seq_len, const int* __restrict__ prefix_len,
-    const int* __restrict__ page_table, int max_pages, int n_seq, int n_tokens, int n_q, int n_kv, int n_pool_pages, int row_blocks, int parts,
-    int min_parts, float scale_log2e, float* __restrict__ part_o, float* __restrict__ part_ml) {
+    const int* __restrict__ page_table, int max_pages, int n_seq, int n_tokens, int n_q, int n_kv, int n_pool_pages, int row_blocks, int more_rows,
+    int parts, int min_parts, float scale_log2e, float* __restrict__ part_o, float* __restrict__ part_ml) {
     constexpr int AHEAD = KV8 && NR == 1 ? 2 : 1;   // steps whose loads are on their way behind the one that is worked on
     constexpr int KS = HD / 32;        // matrix instructions of a page's scores
     constexpr int DL = HD / 16;        // head_dim indices of a lane of V, and of the result's 16 rows each
@@ -128,15 +128,23 @@ __global__ __launch_bounds__(WAVES * 64, NR == 1 && !KV8 ? 3 : 2) void attn_rows
     // Workgroup b runs on XCD b % 8.  The kv heads of a (sequence, part, row block) go to one XCD side by side: a page's heads are
     // neighbours in memory and a block is 8.5 (4.25) lines of 128 bytes, so that each fetches a line that the next one needs too.
     const int G = n_q / n_kv;
-    int kvh = blockIdx.x / 8 % n_kv, rest = blockIdx.x / 8 / n_kv * 8 + blockIdx.x % 8, rb0 = rest % row_blocks;
-    rest /= row_blocks;
+    int bid = blockIdx.x, rb0 = 0;
+    if constexpr (KV8 && NR > 1) {   // the launch several times over, for the last row_blocks blocks of a sequence first
+        const int launch = gridDim.x / more_rows;
+        rb0 = (more_rows - 1 - bid / launch) * row_blocks;
+        bid %= launch;
+    }
+    int kvh = bid / 8 % n_kv, rest = bid / 8 / n_kv * 8 + bid % 8;
     if constexpr (KV8 && NR > 1) {
         const RowsGroups grp(n_seq * parts * n_kv, row_blocks);
-        const int at = blockIdx.x / 8, unit = at / grp.blocks * 8 + blockIdx.x % 8;
-        rb0 = unit % grp.n + at % grp.blocks * grp.n;
-        if (rb0 >= row_blocks) return;
+        const int at = bid / 8, unit = at / grp.blocks * 8 + bid % 8, rb = unit % grp.n + at % grp.blocks * grp.n;
+        if (rb >= row_blocks) return;
+        rb0 += rb;
         kvh = unit / grp.n % n_kv;
         rest = unit / grp.n / n_kv;
+    } else {
+        rb0 = rest % row_blocks;
+        rest /= row_blocks;
     }
     const int part = rest % parts, seq = rest / parts;
     if (seq >= n_seq) return;
@@ -159,7 +167,7 @@ __global__ __launch_bounds__(WAVES * 64, NR == 1 && !KV8 ? 3 : 2) void attn_rows
     asm volatile("" : "+v"(kv8_lane_s));
     const int v_chunk = HD == 128 ? i : i >> 1, v_group = i / (KV4_GROUP / DL), o_group = g * 4 * DL / KV4_GROUP;
 
-    for (int rb = rb0; rb * ROWS < n_rows; rb += row_blocks) {
+    for (int rb = rb0; rb * ROWS < n_rows; rb += KV8 && NR > 1 ? row_blocks * more_rows : row_blocks) {
         const int last_row = rb * ROWS + ROWS - 1 < n_rows ? rb * ROWS + ROWS - 1 : n_rows - 1;
         const int vis_min = r.H + rb * ROWS / G, kv_end = r.H + last_row / G + 1;  // seen by every row, by the last row
         int limit[NR];                                                             // last key this lane's rows see
@@ -607,11 +615,11 @@ int launch_rows(const RowsAttn& a, const RowsPlan& p, float* part, hipStream_t s
     if (KV8 && p.row_tiles > 1) {
         const int units = a.n_seq * p.parts * a.n_kv;
         const RowsGroups grp(units, p.row_blocks);
-        wgs = (units * grp.n + 7) / 8 * 8 * grp.blocks;
+        wgs = (units * grp.n + 7) / 8 * 8 * grp.blocks * p.more_rows;
     }
     hipLaunchKernelGGL(kern, dim3(wgs), dim3(WAVES * 64), 0, s, a.q, a.out, a.k_pool,
                        a.v_pool, a.cu, a.seq_len, a.prefix_len, a.page_table, a.max_pages, a.n_seq, a.n_tokens, a.n_q, a.n_kv, a.n_pool_pages,
-                       p.row_blocks, p.parts, p.min_parts, scale_log2e, part, part_ml);
+                       p.row_blocks, p.more_rows, p.parts, p.min_parts, scale_log2e, part, part_ml);
     LAPS_LAUNCH_CHECK();
     const int rows = (a.n_tokens + a.n_seq - 1) / a.n_seq;   // of a sequence, in the mean
     if (p.parts > FEW_PARTS) {
@@ -665,7 +673,13 @@ RowsPlan laps_attn_rows_plan(int bits, int n_seq, int n_tokens, int n_q, int n_k
     // over 2000 / 4000 / 8000 19.2 / 29.5 / 54.7 by the rule, 15.9 / 27.0 / 50.5 in 1.  One long history among short ones keeps
     // the parts that the batch leaves it: 32B, 95 tokens over 100 to 2000 keys and one over 100000 274 in 2 parts, 114 in 16, with
     // which the same table without a long one takes 76 instead of 42.
-    if (rounds <= 8) return {tiles, (int)blocks, 1, 1};
+    // 8 bits: as many workgroups again for the longer turns of a ragged batch, ahead of the others, where they find nothing to do in an even
+    // one.  With / without: 32B, five draws of 16 turns of 17 to 64 tokens over 512 to 4096 keys 84 / 82, 86 / 104, 93 / 97, 90 / 104, 70 / 75 us, 12 of
+    // 9 to 100 over 100 to 3000 59 / 68, 40 of 4 to 20 over 20 to 2000 45 / 52; 7B, 20 of 8 to 40 over 64 to 10000 103 / 117; even ones the same but
+    // 64 of 8 tokens over 2000 keys 78 / 74.  Behind the others 89, 93, 91, 85, 61 and 60, 46, 109; beside the blocks of the same keys they
+    // cost even batches half their time (64 of 8 over 2000 110); three and four times as many are like two.
+    const int more_rows = bits == 8 && tiles == 2 && n_seq > 1 && blocks * n_seq * n_kv <= (1 << 18) ? 2 : 1;
+    if (rounds <= 8) return {tiles, (int)blocks, more_rows, 1, 1};
     const long units = blocks * n_seq * n_kv, places = tiles == 1 ? (bits == 8 ? 512 : 768) : 256;
     auto within = [](long n, long most) { return n < most ? (n > 1 ? n : 1) : most; };
     const long min_parts = within(within(places / units, rounds / 2), MAX_PARTS);
@@ -674,7 +688,7 @@ RowsPlan laps_attn_rows_plan(int bits, int n_seq, int n_tokens, int n_q, int n_k
     // 163 / 127 / 141; two over 100000 in 51 by each.
     const long more = tiles == 2 ? 1024 : bits == 4 ? 1536 : units < 512 ? 1024 : 1;
     const long parts = within(within(more / units, rounds / (tiles == 1 ? 16 : 10)), MAX_PARTS);
-    return {tiles, (int)blocks, (int)(parts > min_parts ? parts : min_parts), (int)min_parts};
+    return {tiles, (int)blocks, more_rows, (int)(parts > min_parts ? parts : min_parts), (int)min_parts};
 }
 
 size_t laps_attn_rows_bytes(const RowsPlan& p, int n_tokens, int n_q, int hd) {

@@ -697,7 +697,7 @@ static int kvq_plan_info(const char* who, int bits, int n_seq, int n_tokens, int
     if (laps_attn_takes_rows(n_seq, n_tokens, n_q_heads, n_kv_heads)) {
         const RowsPlan p = laps_attn_rows_plan(bits, n_seq, n_tokens, n_q_heads, n_kv_heads, max_pages);
         out[0] = 16 * p.row_tiles;
-        out[1] = p.row_blocks;
+        out[1] = p.row_blocks * p.more_rows;
         out[2] = p.parts;
         out[3] = p.min_parts;
         out[4] = 0;

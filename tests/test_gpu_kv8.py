@@ -239,7 +239,8 @@ def test_head_layouts(heads):
 # fill their groups and that do not
 @pytest.mark.parametrize("heads,new,pre", [((16, 1, 128), [100], [300]), ((16, 1, 128), [33, 70, 2], [5, 900, 64]), ((4, 2, 64), [200], [100]),
                                            ((40, 8, 128), [90], [2500]), ((28, 4, 128), [5] * 9, [100, 0, 700, 64, 65, 31, 32, 33, 1]),
-                                           ((40, 8, 128), [13, 1, 40, 0, 7, 22, 9], [70, 300, 0, 5, 1900, 16, 15])])
+                                           ((40, 8, 128), [13, 1, 40, 0, 7, 22, 9], [70, 300, 0, 5, 1900, 16, 15]),
+                                           ((28, 4, 128), [1] * 20 + [90], list(range(0, 420, 20)))])      # one turn of many times the mean
 def test_row_blocks_of_the_same_keys(heads, new, pre):
     n_q, n_kv, hd = heads
     b = Batch(inputs.ModelCfg(256, n_q, n_kv, hd, 512, 1), new, pre, spare=3, seed=n_q + len(new)).write()
