@@ -834,17 +834,15 @@ static bool fp8_shape(int m, int n, int k) {
     return blocks * fp8_pitch(m) < (1L << 31) && blocks * fp8_pitch(n) < (1L << 31) && ((long)m + 255) / 256 * (((long)n + 255) / 256) <= (1L << 22);
 }
 
-static size_t fp8_partial_bytes(int m, int n, int k) {
-    const Fp8Plan p = laps_fp8_plan(m, n, (int)fp8_columns(k));
-    return p.split > 1 ? align256((size_t)p.split * m * n * sizeof(float)) : 0;
-}
+static Fp8Plan fp8_plan_of(int m, int n, int k) { return laps_fp8_plan(m, n, (int)fp8_columns(k)); }
+static size_t fp8_partial_bytes(const Fp8Plan& p, int m, int n) { return p.split > 1 ? align256((size_t)p.split * m * n * sizeof(float)) : 0; }
 
 extern "C" int laps_gemm_fp8_plan_info(int32_t m, int32_t n, int32_t k, int32_t* out) {
     if (!out || !fp8_shape(m, n, k)) {
         laps_set_error("gemm_fp8_plan_info: NULL output or unsupported shape (m=%d n=%d k=%d)", m, n, k);
         return LAPS_EINVAL;
     }
-    const Fp8Plan p = laps_fp8_plan(m, n, (int)fp8_columns(k));
+    const Fp8Plan p = fp8_plan_of(m, n, k);
     laps_fp8_tile_dims(p.cfg, &out[0], &out[1]);
     out[2] = p.split;
     out[3] = p.per * FP8_BLOCK;
@@ -852,7 +850,24 @@ extern "C" int laps_gemm_fp8_plan_info(int32_t m, int32_t n, int32_t k, int32_t*
     return LAPS_OK;
 }
 
-extern "C" size_t laps_gemm_fp8_workspace_bytes(int32_t m, int32_t n, int32_t k) { return fp8_shape(m, n, k) ? fp8_partial_bytes(m, n, k) : 0; }
+extern "C" size_t laps_gemm_fp8_workspace_bytes(int32_t m, int32_t n, int32_t k) {
+    return fp8_shape(m, n, k) ? fp8_partial_bytes(fp8_plan_of(m, n, k), m, n) : 0;
+}
+
+static int fp8_check_product(const char* who, const laps_ctx* c, const void* a, const void* a_scales, const void* w, const void* w_scales, const void* out) {
+    if ((((uintptr_t)a | (uintptr_t)a_scales | (uintptr_t)w | (uintptr_t)w_scales) & 15) || ((uintptr_t)out & 1)) {
+        laps_set_error("%s: codes and scales must be 16-byte aligned", who);
+        return LAPS_EINVAL;
+    }
+    return check_current_device(c, who);
+}
+
+static int fp8_product(const Fp8Plan& p, const void* a, const void* a_scales, const void* w, const void* w_scales, void* out, int m, int n, int k,
+                       void* partial, void* stream) {
+    return laps_launch_gemm_fp8(p, static_cast<const unsigned char*>(a), static_cast<const unsigned char*>(a_scales),
+                                static_cast<const unsigned char*>(w), static_cast<const unsigned char*>(w_scales), static_cast<bf16_t*>(out), m, n,
+                                (int)fp8_columns(k), static_cast<float*>(partial), static_cast<hipStream_t>(stream));
+}
 
 extern "C" int laps_gemm_fp8(laps_ctx* c, const void* a, const void* a_scales, const void* w, const void* w_scales, void* out, int32_t m,
                              int32_t n, int32_t k, void* ws, size_t ws_bytes, void* stream) {
@@ -860,33 +875,27 @@ extern "C" int laps_gemm_fp8(laps_ctx* c, const void* a, const void* a_scales, c
         laps_set_error("gemm_fp8: NULL pointer or unsupported shape (m=%d n=%d k=%d)", m, n, k);
         return LAPS_EINVAL;
     }
-    if ((((uintptr_t)a | (uintptr_t)a_scales | (uintptr_t)w | (uintptr_t)w_scales) & 15) || ((uintptr_t)out & 1)) {
-        laps_set_error("gemm_fp8: codes and scales must be 16-byte aligned");
-        return LAPS_EINVAL;
-    }
-    LAPS_TRY(check_current_device(c, "gemm_fp8"));
-    const size_t need = fp8_partial_bytes(m, n, k);
+    LAPS_TRY(fp8_check_product("gemm_fp8", c, a, a_scales, w, w_scales, out));
+    const Fp8Plan p = fp8_plan_of(m, n, k);
+    const size_t need = fp8_partial_bytes(p, m, n);
     if (need > 0 && (!ws || ws_bytes < need || ((uintptr_t)ws & 255))) {
         laps_set_error("gemm_fp8: this shape splits K and needs %zu bytes of 256-byte aligned workspace", need);
         return LAPS_ENOMEM;
     }
-    const int columns = (int)fp8_columns(k);
-    return laps_launch_gemm_fp8(laps_fp8_plan(m, n, columns), static_cast<const unsigned char*>(a), static_cast<const unsigned char*>(a_scales),
-                                static_cast<const unsigned char*>(w), static_cast<const unsigned char*>(w_scales), static_cast<bf16_t*>(out), m, n,
-                                columns, static_cast<float*>(ws), static_cast<hipStream_t>(stream));
+    return fp8_product(p, a, a_scales, w, w_scales, out, m, n, k, ws, stream);
 }
 
 // Workspace of a projection of bf16 rows: their codes and scales, then the product's.
-static void linear_layout(int m, int n, int k, size_t* scales, size_t* partial, size_t* total) {
+static void linear_layout(const Fp8Plan& p, int m, int n, int k, size_t* scales, size_t* partial, size_t* total) {
     *scales = align256((size_t)m * fp8_columns(k));
     *partial = *scales + align256((size_t)(fp8_columns(k) / FP8_BLOCK) * fp8_pitch(m));
-    *total = *partial + fp8_partial_bytes(m, n, k);
+    *total = *partial + fp8_partial_bytes(p, m, n);
 }
 
 extern "C" size_t laps_linear_fp8_workspace_bytes(int32_t m, int32_t n, int32_t k) {
     if (!fp8_shape(m, n, k)) return 0;
     size_t scales, partial, total;
-    linear_layout(m, n, k, &scales, &partial, &total);
+    linear_layout(fp8_plan_of(m, n, k), m, n, k, &scales, &partial, &total);
     return total;
 }
 
@@ -896,25 +905,25 @@ extern "C" int laps_linear_fp8(laps_ctx* c, const void* x, const void* w, const 
         laps_set_error("linear_fp8: NULL pointer, unaligned workspace or unsupported shape (m=%d n=%d k=%d)", m, n, k);
         return LAPS_EINVAL;
     }
+    LAPS_TRY(fp8_check_product("linear_fp8", c, ws, ws, w, w_scales, out));
+    if ((uintptr_t)x & 1) {
+        laps_set_error("linear_fp8: rows must be aligned to their elements");
+        return LAPS_EINVAL;
+    }
+    const Fp8Plan p = fp8_plan_of(m, n, k);
     size_t scales, partial, total;
-    linear_layout(m, n, k, &scales, &partial, &total);
+    linear_layout(p, m, n, k, &scales, &partial, &total);
     if (ws_bytes < total) {
         laps_set_error("linear_fp8: workspace too small (%zu < %zu bytes)", ws_bytes, total);
         return LAPS_ENOMEM;
     }
     const bf16_t* rows = static_cast<const bf16_t*>(x);
-    if (laps_fp8_takes_bf16_rows(laps_fp8_plan(m, n, (int)fp8_columns(k)), rows, m, k)) {
-        if ((((uintptr_t)w | (uintptr_t)w_scales) & 15) || ((uintptr_t)out & 1)) {
-            laps_set_error("linear_fp8: codes and scales must be 16-byte aligned");
-            return LAPS_EINVAL;
-        }
-        LAPS_TRY(check_current_device(c, "linear_fp8"));
+    if (laps_fp8_takes_bf16_rows(p, rows, m, k))
         return laps_launch_linear_fp8_rows(rows, static_cast<const unsigned char*>(w), static_cast<const unsigned char*>(w_scales),
                                            static_cast<bf16_t*>(out), m, n, k, static_cast<hipStream_t>(stream));
-    }
     unsigned char* w8 = static_cast<unsigned char*>(ws);
-    LAPS_TRY(laps_fp8_quant(c, x, m, k, w8, w8 + scales, stream));
-    return laps_gemm_fp8(c, w8, w8 + scales, w, w_scales, out, m, n, k, w8 + partial, ws_bytes - partial, stream);
+    LAPS_TRY(laps_launch_fp8_quant(rows, m, k, w8, w8 + scales, static_cast<hipStream_t>(stream)));
+    return fp8_product(p, w8, w8 + scales, w, w_scales, out, m, n, k, w8 + partial, stream);
 }
 
 extern "C" size_t laps_gemm_workspace_bytes(int32_t m, int32_t n, int32_t k, int32_t split_k) {

@@ -282,6 +282,21 @@ def test_more_rows_than_the_library_counts(ctx):
         ctx.laps_fp8_quant(x)
 
 
+def test_projections_refuse_what_their_parts_would(ctx):
+    """Rows off their elements' bounds, weights and scales off 16 bytes, results off two: before any launch, on both paths."""
+    L, h = api.lib(), ctx._h
+    for m, n, k in ((3, 40, 256), (200, 300, 512)):
+        x = torch.zeros(m * k + 1, dtype=torch.bfloat16, device="cuda")
+        w, sw, ws = (torch.zeros(s, dtype=torch.uint8, device="cuda") for s in (n * k + 16, k // 128 * 304 + 16, L.laps_linear_fp8_workspace_bytes(m, n, k)))
+        y = torch.full((m * n + 1,), 2.0, dtype=torch.bfloat16, device="cuda")
+        ptr = [t.data_ptr() for t in (x, w, sw, y)]
+        for at, off in ((0, 1), (1, 8), (2, 4), (3, 1)):
+            a = [p + off * (i == at) for i, p in enumerate(ptr)]
+            assert L.laps_linear_fp8(h, *a, m, n, k, ws.data_ptr(), ws.numel(), None) == -1, (m, at)
+        torch.cuda.synchronize()
+        assert (y == 2).all()
+
+
 def test_results_repeat_on_any_stream(ctx):
     g = np.random.default_rng(3)
     a, w = O.quantise(g.standard_normal((48, 5120))), O.quantise(g.standard_normal((512, 5120)))
