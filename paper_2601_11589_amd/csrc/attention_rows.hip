@@ -109,7 +109,7 @@ struct RowsGroups {
 // NR: blocks of 16 rows that share what is read and unpacked.
 // Waves a SIMD: as many as registers allow, 3 (4 bits, one block) or 2.  8 bits have twice the pieces of a step in registers; with one block
 // they go two steps ahead at 2 waves rather than one step ahead at 3: 32B, 64 tokens over 4096 keys each 112 -> 98 us, over 512 to
-// 8191 130 -> 114 (the loads alone, without the work on them, take 92 of the first).
+// 8191 130 -> 114 (two and three parts a sequence; the loads alone, without the work on them, took 92 of the first).
 // Four blocks that share what is unpacked, at one wave a SIMD, are not kept: 32B, 16 sequences of 17 to 64 tokens over 512 to 4096 keys
 // 88 us and, with the next step's scores among this one's exponentials, 92; two blocks 78.
 template <int HD, int NR, bool KV8>
