@@ -92,8 +92,14 @@ __device__ __forceinline__ int key_a(int row) { return (row >> 1) & 7; }
 __device__ __forceinline__ int key_w(int row) { return ((row >> 1) & 1) | (((row >> 3) & 3) << 1); }
 
 // The matrix instructions are inline assembly: the builtin has separate accumulator operands in and out, and the register allocator
-// fills the loop with moves between them.  The compiler therefore does not know the wait states between them and what else touches
-// their accumulators; every accumulator passes through a statement behind the wait.
+// fills the loop with moves between them.  The compiler therefore does not know the wait states round them:
+//   * what else touches their accumulators: every accumulator passes through acc_fence before the loop and behind it;
+//   * two behind a vector instruction that writes a code or a scale.  Codes come straight from LDS.  Scales are bytes, which the compiler
+//     zero-extends with an instruction of its own, at the head of the loop for those that came over its end; so each is pinned as a whole
+//     register at the end of the quadrant that reads it, two wait states before the next.  (Two in front of every matrix instruction
+//     instead cost 1 to 3.5 %: 4096 x 3584 x 3584 49.6 -> 51.2 us, 2048 x 55296 x 5120 447 -> 452; like this 49.7 and 446.)
+// That nothing else of the kind stands in the loops is looked up in the assembly by tests/test_matrix_asm_waits_host.py; run it, and the exact
+// products on every tile, after a change of compiler or flags.
 template <typename S>
 __device__ __forceinline__ void acc_fence(f32x4 (&acc)[S::MI][S::NI]) {
     asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
@@ -301,6 +307,9 @@ __device__ __forceinline__ void gemm_tile(const Fp8Args& g, unsigned char* smem)
             }
             __builtin_amdgcn_sched_barrier(0);
         }
+#pragma unroll
+        for (int i = 0; i < (rd_a() ? MH : NH); ++i) asm volatile("" : "+v"(rd_a() ? ea[rh() * MH + i] : eb[rh() * NH + i]));
+        asm volatile("s_nop 1");
     };
     auto half_end = [&]() {
         dma_barrier<(NS - 2) * S::LOADS>();
