@@ -187,6 +187,22 @@ def test_products_within_their_roundings(ctx, m, n, k):
     assert off <= ULP / math.sqrt(3) + 2.0 ** -13, off      # bf16 roundings alone: at most ULP / sqrt(3) in the mean square
 
 
+@pytest.mark.parametrize("m,n,k", [(1, 4000, 3584), (33, 520, 5120), (150, 260, 1408), (300, 600, 18944), (520, 1100, 256)])
+def test_products_are_as_near_as_documented(ctx, m, n, k):
+    """The cuts take 3e-5 of a result at the most, in the mean square of a row, and float32 sums a tenth of that.  So an element is off by half
+    a bf16 step of its value and 8 times that; and it differs from the 64-bit value's own rounding where a border between two numbers of
+    bf16 lies between the two, once in (step / error): of as many elements as the sum of these, within four standard deviations."""
+    g = np.random.default_rng(m + n)
+    a, w = O.quantise(g.standard_normal((m, k))), O.quantise(g.standard_normal((n, k)) * 0.02)
+    got, want = wide(product(ctx, a, w)), exact(a, w)
+    error = 3e-5 * np.sqrt((want ** 2).mean(1, keepdims=True))
+    step = np.exp2(np.floor(np.log2(np.maximum(np.abs(want), np.abs(got)))) - 7)
+    assert (np.abs(got - want) <= step / 2 + 8 * error).all()
+    expected = np.minimum(1, error / step).sum()
+    differ = (got != wide(torch.from_numpy(want).to(torch.float32).to(torch.bfloat16))).sum()
+    assert differ <= expected + 4 * math.sqrt(expected), (differ, expected)
+
+
 def test_a_nan_makes_its_row_and_its_column(ctx):
     g = np.random.default_rng(2)
     a, w = whole_numbers(g, 150, 300, 2), whole_numbers(g, 260, 300, 2)

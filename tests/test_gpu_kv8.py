@@ -311,6 +311,20 @@ def test_rows_without_a_token_stay_in_blocks(name, rows):
     b.ctx.close()
 
 
+# Decode batches with one turn that a workgroup walks block after block: (heads, tokens of each sequence, rows of a block)
+@pytest.mark.parametrize("heads,new,rows", [((4, 2, 64), [1] * 70 + [450], 16), ((28, 4, 128), [1] * 40 + [150] + [1] * 79, 16),
+                                            ((40, 8, 128), [350] + [1] * 95, 32), ((28, 4, 128), [1] * 30 + [300, 0] + [1] * 29, 32)])
+def test_single_tokens_and_one_long_turn(heads, new, rows):
+    n_q, n_kv, hd = heads
+    g = np.random.default_rng(len(new))
+    pre = np.where(np.asarray(new) > 1, 333, g.integers(0, 120, len(new)))
+    b = Batch(inputs.ModelCfg(256, n_q, n_kv, hd, 512, 1), new, pre, spare=3, seed=len(new)).write()
+    p = plan(b)
+    assert p[0] == rows and p[1] * rows < max(new) * n_q // n_kv, p
+    b.check(b.attend())
+    b.ctx.close()
+
+
 def test_many_sequences():
     g = np.random.default_rng(8)
     b = Batch(inputs.tiny_cfg(1), g.integers(0, 3, 700), g.integers(0, 90, 700)).write()
