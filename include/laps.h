@@ -386,7 +386,8 @@ int laps_attention_kv4(laps_ctx* ctx, int32_t n_seq, int32_t n_tokens, const int
                        void* out_dev, void* workspace_dev, size_t workspace_bytes, void* stream);
 
 /* The same over 8-bit pools of n_pages pages (laps_kv8_scatter); page ids outside [0, n_pages) are treated as unset.  A NaN that the cache
- * holds reaches the rows that see its token, in the whole head, and no others.  Workspace, errors and the mean of new tokens as there. */
+ * holds reaches the rows that see its token, in the whole head, and no others.  Workspace, errors and the mean of new tokens as there.
+ * Both lay their work out by the mean of the sequences' new tokens: single tokens and a long turn are faster in a call each. */
 size_t laps_attention_kv8_workspace_bytes(const laps_ctx* ctx, int32_t n_seq, int32_t n_tokens, int32_t max_pages);
 int laps_attention_kv8(laps_ctx* ctx, int32_t n_seq, int32_t n_tokens, const int32_t* cu_seqlens_dev, const int32_t* seq_len_dev,
                        const int32_t* prefix_len_dev, const int32_t* page_table_dev, int32_t max_pages, int32_t n_pages,
@@ -403,7 +404,8 @@ size_t laps_gemm_fp8_workspace_bytes(int32_t m, int32_t n, int32_t k);
 int laps_gemm_fp8(laps_ctx* ctx, const void* a_dev, const void* a_scales_dev, const void* w_dev, const void* w_scales_dev, void* out_dev,
                   int32_t m, int32_t n, int32_t k, void* workspace_dev, size_t workspace_bytes, void* stream);
 /* A projection of bf16 rows: laps_fp8_quant of x [m, k] into the workspace (laps_linear_fp8_workspace_bytes(m, n, k) bytes, 256-byte
- * aligned), then laps_gemm_fp8. */
+ * aligned), then laps_gemm_fp8.  k is that of the rows; the weights have laps_fp8_columns(k) columns, and nothing tells how many of the last
+ * 128 their own k had: values behind the rows' k are multiplied by zeros. */
 size_t laps_linear_fp8_workspace_bytes(int32_t m, int32_t n, int32_t k);
 int laps_linear_fp8(laps_ctx* ctx, const void* x_dev, const void* w_dev, const void* w_scales_dev, void* out_dev, int32_t m, int32_t n,
                     int32_t k, void* workspace_dev, size_t workspace_bytes, void* stream);

@@ -675,7 +675,8 @@ class LapsCtx:
         return y
 
     def laps_linear_fp8(self, x, w, w_scales, out=None, stream=None):
-        """bf16 [m, n] = x w^T: laps_fp8_quant of the bf16 rows x [m, k], then laps_gemm_fp8."""
+        """bf16 [m, n] = x w^T: laps_fp8_quant of the bf16 rows x [m, k], then laps_gemm_fp8.  w holds laps_fp8_columns(k) codes a row: of
+        weights that were longer than x by up to 127, the columns past k are multiplied by zeros without a word."""
         (m, k), device = x.shape, w.get_device()
         self._fp8_pitch("x", m)
         x_p = _expect("x", x, torch.bfloat16, (m, k), device)

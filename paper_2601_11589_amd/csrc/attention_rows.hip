@@ -2,10 +2,10 @@
 //
 //   O = softmax(Q K^T / sqrt(hd)) V over the cached keys, row t of a sequence seeing keys <= H + t
 //
-// One pass over the keys with a running maximum and sum a row.  What bounds it is the cache: 8.5 * hd bytes of K and as many of V for
-// 16 keys of a kv head, and 4 * 16 * hd flops for each of the G query heads that share them.  So nothing is staged: a wave walks the
-// keys 32 at a time (two pages), and every load is one 16-byte piece a lane, 1 KB of a page a wave, straight into the
-// operand registers of 16x16x32 matrix instructions:
+// One pass over the keys with a running maximum and sum a row.  What bounds it is the cache: 8.5 * hd bytes of K in 4 bits, 16 * hd in 8, and
+// as many of V for 16 keys of a kv head, and 4 * 16 * hd flops for each of the G query heads that share them.  So nothing is staged: a wave
+// walks the keys 32 at a time (two pages), and every load is one 16-byte piece a lane, 1 KB of a page a wave, straight into the
+// operand registers of 16x16x32 matrix instructions.  Over 4 bits:
 //
 //   S^T = K Q^T   lane (i, g) = (lane % 16, lane / 16) holds key i and head_dim indices hd/4 g .. hd/4 g + hd/4 - 1: its piece of the page
 //                 [16 keys][hd / 2 bytes].  Which index is which of the instruction's 32 does not matter as long as Q's registers agree.
@@ -13,7 +13,7 @@
 //                 share of the second product's 32 keys, and V's pages are laid out for that: [hd / 8][16 keys][8 values], four keys of
 //                 the same eight (hd 64: four) head_dim indices a lane.  No value changes lanes.
 //
-// Codes become bf16 operands exactly (one instruction a pair, the group's scale included; two permutes a pair of V's to bring keys
+// Codes become bf16 operands exactly (one instruction a pair, the scale included; over 4 bits two permutes a pair of V's to bring keys
 // side by side).  The query rows are the G heads of a kv head for each of the sequence's new tokens, 16 a block.
 // Weights are rounded to bf16, which the second product takes, and their sum is that of the rounded ones, so that they add up to one; scores,
 // sums, O and partial results are float32.  That makes outputs 1.1 to 1.4 times as far from 64 bits as float32 weights would (1.8e-3 to
@@ -56,6 +56,7 @@ __device__ __forceinline__ bool seq_range(int seq, const int* cu, const int* seq
     return true;
 }
 
+// Of either cache, whatever the name.
 __device__ __forceinline__ int part_steps(int kv_len, int max_pages, int parts, int min_parts, int* used) {
     return laps_kv4_part_rounds(kv_len, max_pages, parts, min_parts, used) * WAVES;
 }
@@ -77,7 +78,8 @@ struct Piece<HD, true> {
 // O += V^T P^T.  8-bit pools: by hand, with one operand for what O was and what it is.  The builtin has two, and with twice the pieces of a
 // step in registers the allocator no longer gets by without moves and spills: two blocks of rows 25 spills at 2 waves a SIMD, now none.
 // The compiler does not know what such an instruction needs before and behind it: the two wait states behind vector instructions that
-// made its operands stand here, those before O is used otherwise are o_settle's.
+// made its operands stand here, those before O is used otherwise are o_settle's.  That O is not moved between the bodies of the loop, where no
+// o_settle stands, is looked up in the assembly by tests/test_matrix_asm_waits_host.py: run it after a change of compiler or flags.
 template <bool KV8>
 __device__ __forceinline__ void add_product(f32x4& o, bf16x8 v, bf16x8 p) {
     if constexpr (KV8) asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(o) : "v"(v), "v"(p));
@@ -204,8 +206,8 @@ __global__ __launch_bounds__(WAVES * 64, NR == 1 && !KV8 ? 3 : 2) void attn_rows
             ids = (id > 0 && id < n_pool_pages) ? id : 0;      // unset, or not a page of the pool
             asm volatile("" : "+v"(ids));   // waited for here: behind the join it would be waited for at every step, with all loads in flight
         };
-        // Up to 16 rows a sequence: keys are read once and past the caches, 2.3 GB 418 -> 378 us (6.0 TB/s; 280 MB that the memory-side cache
-        // held from the call before 52 -> 58).  More rows: other blocks of theirs read the same keys.
+        // 4 bits, up to 16 rows a sequence: keys are read once and past the caches, 2.3 GB 418 -> 378 us (6.0 TB/s; 280 MB that the memory-side
+        // cache held from the call before 52 -> 58).  More rows: other blocks of theirs read the same keys.
         auto codes = [](const auto* from) { return NR == 1 ? __builtin_nontemporal_load(from) : *from; };
         // 8-bit pools: steps past the last one go through descriptors of no bytes, which takes no request.
         auto load = [&](int n, Piece<HD, KV8>& x) {
@@ -218,7 +220,9 @@ __global__ __launch_bounds__(WAVES * 64, NR == 1 && !KV8 ? 3 : 2) void attn_rows
                     const size_t at = (size_t)page * kv8_page(n_kv, HD) + (size_t)kvh * kv8_codes(HD);
                     auto block = [&](const byte_t* pool) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<byte_t*>(pool + at), 0, bytes, 0x00020000); };
                     const __amdgpu_buffer_rsrc_t kb = block(k_pool), vb = block(v_pool);
-                    constexpr int PAST = NR == 1 ? 2 : 0;   // nt, as below
+                    // past the caches (nt) V alone, on the same terms: a load of K takes (head_dim 128) 64 bytes of each of its 128-byte lines, and
+                    // the other half would be fetched again
+                    constexpr int PAST = NR == 1 ? 2 : 0;
 #pragma unroll
                     for (int u = 0; u < HD / 64; ++u) {
                         x.k[p][u] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kb, kv8_lane_k + u * 64, 0, 0));
@@ -646,7 +650,9 @@ int launch_rows(const RowsAttn& a, const RowsPlan& p, float* part, hipStream_t s
 // 16000 323 and 262, 4 of 200 318 and 276).  Fewer than 256 workgroups of 128 rows have no blocks to go to: over bf16 pools their key ranges are
 // split.  And rows count by their mean: a long turn among single tokens is walked block after block by the few workgroups of
 // a sequence (32B, 95 tokens over 512 to 8100 keys 98 us, a turn of 350 over 4000 65, both in one call 1620, in blocks 363; 7B,
-// 127 tokens 72, a turn of 900 100, both 3008, in blocks 334).
+// 127 tokens 72, a turn of 900 100, both 3008, in blocks 334).  8 bits, the same lengths: 165, 72 and 1011; 131, 119 and 1992; where the
+// mean is up to 16 rows there are no surplus workgroups either (7B, 239 tokens over 512 to 4096 keys 109, a turn of 300 over 4000 53, both 3532).
+// Two calls, one for the tokens and one for the turn, take the sum of theirs.
 // 8 bits, this kernel / blocks: 32B, 16 sequences of 17 to 64 tokens over 512 to 4096 keys 78 / 81 us, 16 of 64 over 2048 76 / 81, 64 of 8 / 16 /
 // 32 over 2000 71 / 94 / 144 and 87 / 95 / 152, 4 of 200 over 16000 359 / 294; 7B, 12 of 60 to 120 over 100 to 3000 75 / 72.
 bool laps_attn_takes_rows(int n_seq, int n_tokens, int n_q, int n_kv) {
